@@ -55,7 +55,7 @@ def listed():
         _attend(name="attend_one_user", len_min=777, len_max=777, page=16),
         # a generation step of a full batch of ragged contexts: the cache is read once
         _attend(name="attend_decode_batch", batch=64, len_min=1024, len_max=4096),
-        # a chunk of a long document: 2048 new tokens behind 30720 cached ones, odd group of query heads
+        # a chunk of a long document: the last 2048 of 32768 tokens are new, odd group of query heads
         _attend(name="attend_chunk_long", new_min=2048, new_max=2048, len_min=32768, len_max=32768, q_heads=28, kv_heads=4, page=128),
         # a mixed batch of a small model: some sequences decode, others bring a chunk
         _attend(name="attend_mixed_batch", batch=64, new_min=1, new_max=512, len_min=512, len_max=2048, q_heads=16, kv_heads=16, head_dim=64,
