@@ -33,7 +33,8 @@
  *    Argument errors are returned before anything is launched.  A device-side wait
  *    that runs out (every wait in the kernels is bounded) records SEKA_ERR_TIMEOUT in
  *    the first word of `workspace`; seka_poll_status reads it.
- *  - Causal, forward only, queries and keys of equal length.  head_dim is 64 or 128.
+ *  - Causal, forward only; queries and keys of equal length (the paged cache: the queries are the last tokens).  head_dim is
+ *    64 or 128.
  */
 #ifndef SEKA_H_
 #define SEKA_H_
@@ -235,6 +236,119 @@ seka_status seka_learn_projections(const seka_learn_shape* shape, const void* h,
                                    float* omega_pos, float* omega_neg, float* U_pos, float* U_neg,
                                    float* S_pos, float* S_neg, int32_t* k_pos, int32_t* k_neg, float* D,
                                    void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * ---------------------------------------------------------------- paged cache
+ * The calls below serve steered prompts from a key/value cache kept in pages.  A step of a server for one layer is: seka_edit_keys
+ * on the new keys (the hook works on the keys as the projection gives them, before rotation), seka_rope_append (rotation; keys
+ * and values to their pages), seka_paged_attention over the whole cache, for single tokens and for chunks of a prompt; and, where
+ * the cache has to stay bounded, seka_attention_mass behind it and seka_evict_cache now and then, which keeps what
+ * attention used, the latest tokens and the highlighted ones.
+ *
+ *  - K_pages and V_pages are bf16 [n_pages, page_size, Hkv, d], 16-byte aligned.  block_table[b * max_pages + p] is the page of
+ *    cached tokens p * page_size .. of sequence b; entries behind its last token are not read.
+ *  - cache_lens[b] counts the cached tokens of sequence b, the new ones INCLUDED; a sequence holds at most
+ *    cap = max_pages * page_size.
+ *  - New tokens are packed: Q [T, Hq, d] and so on, T = total_new; sequence b owns cu_new[b] .. cu_new[b+1]-1 (cu_new == NULL:
+ *    max_new each).  New token i of n_b is row cache_lens[b] - n_b + i of its cache; a negative row does not
+ *    exist: such a token is padding (nothing is stored for it, it sees no key).  A padded decode batch has cache_lens[b] = 0
+ *    for the idle sequences.
+ *  - Per-row state of the cache (accumulated weight, position) is [B, Hkv, cap], a row per cached token and KV head.  Rows
+ *    behind cache_lens[b] are never read or written.
+ *  - One workspace of seka_paged_workspace_bytes(shape) bytes serves all calls, 256-byte aligned, first 256 bytes the status block.  A
+ *    length, token offset or page number outside its range, found on the device, records SEKA_ERR_INVALID_ARG there; nothing outside
+ *    the buffers is touched, the call's outputs are then undefined.  A launch on a workspace whose status is not SEKA_OK does nothing.
+ *  - Calls that may run at the same time need a workspace each.  No two sequences may own the same page in a call that
+ *    writes pages (seka_rope_append: the pages of the new rows; seka_evict_cache: any page of a sequence that is cut).
+ */
+typedef struct {
+    int32_t batch;              /* number of sequences B (>= 0) */
+    int32_t total_new;          /* T: new tokens of all sequences (with cu_new NULL: batch * max_new) */
+    int32_t max_new;            /* most new tokens of a sequence */
+    int32_t n_q_heads;          /* Hq, a multiple of n_kv_heads, at most 128 per KV head */
+    int32_t n_kv_heads;         /* Hkv */
+    int32_t head_dim;           /* d: 64 or 128 */
+    int32_t page_size;          /* 16, 32, 64, 128 or 256 tokens */
+    int32_t n_pages;            /* pages of the pool */
+    int32_t max_pages;          /* entries of a row of block_table */
+    int32_t dtype;              /* seka_dtype of the queries, keys and values that seka_rope_append takes */
+    float   softmax_scale;      /* 0 means 1/sqrt(head_dim) */
+    const int32_t* block_table; /* device int32 [B, max_pages] */
+    const int32_t* cache_lens;  /* device int32 [B] */
+    const int32_t* cu_new;      /* device int32 [B+1], or NULL */
+} seka_paged_shape;
+
+size_t seka_paged_workspace_bytes(const seka_paged_shape* shape);   /* 0: not supported */
+
+typedef enum { SEKA_ROPE_HALF = 0, SEKA_ROPE_INTERLEAVED = 1 } seka_rope_layout;
+typedef enum { SEKA_SCALE_PLAIN = 0, SEKA_SCALE_LINEAR = 1, SEKA_SCALE_BASE = 2, SEKA_SCALE_WAVELENGTH = 3 } seka_rope_scaling;
+
+typedef struct {
+    int32_t rot_dim;            /* r: the first r elements of a head are rotated (even, 2 .. d) */
+    int32_t layout;             /* seka_rope_layout: pairs (x_i, x_{i + r/2}) or (x_{2i}, x_{2i+1}) */
+    float   magnitude;          /* the rotated elements are multiplied by this too; 0 means 1 */
+    const double* turns;        /* device fp64 [r/2]: turns (angle / 2 pi) of pair i per position */
+} seka_rope;
+
+/*
+ * Turns per position of the r/2 pairs, written to HOST memory (the caller copies them to the device once): base^(-2i/r) / 2 pi,
+ *   LINEAR      divided by `scale` (positions squeezed),
+ *   BASE        with base * scale^(r/(r-2)) as the base (the slowest pair squeezed by `scale`, the fastest left; r > 2),
+ *   WAVELENGTH  divided by `scale` where the pair makes less than low_turns turns over trained_len positions, left where it
+ *               makes more than high_turns, blended linearly in between.
+ */
+seka_status seka_rope_turns(int32_t rot_dim, double base, int32_t scaling, double scale, double trained_len,
+                            double low_turns, double high_turns, double* h_turns);
+
+/*
+ * Rotary positions on the new tokens' queries and keys, in fp32 with one rounding; keys and values go to their pages.
+ *   Q, K, V     dtype of the shape, [T, heads, d] with a stride of q_stride / k_stride / v_stride ELEMENTS between tokens (0:
+ *               packed; slices of one [T, (Hq + 2 Hkv) d] projection need no copy); 16-byte aligned, strides too
+ *   positions   int32 [T] (any sign), or NULL: a token's position is its row in the cache
+ *   Q_out       bf16 [T, Hq, d], written for every token, padding too; may be Q itself where that is packed bf16
+ *   pos_cache   int32 [B, Hkv, cap] or NULL: receives the position of the new rows for every KV head
+ * rope == NULL: nothing is rotated.  The angle is reduced in fp64, so positions far out keep their phase.
+ */
+seka_status seka_rope_append(const seka_paged_shape* shape, const seka_rope* rope, const void* Q, int64_t q_stride,
+                             const void* K, int64_t k_stride, const void* V, int64_t v_stride, const int32_t* positions,
+                             void* Q_out, void* K_pages, void* V_pages, int32_t* pos_cache,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Attention of the new tokens over the paged cache: new token i of sequence b sees the rows j <= cache_lens[b] - n_b + i,
+ *     O[t, hq, :] = sum_j softmax_j(Q[t, hq, :] . K[j, hq / (Hq/Hkv), :] * scale) V[j, hq / (Hq/Hkv), :]
+ * Q and O are bf16 [T, Hq, d] (O may be Q), lse, if not NULL, fp32 [T, Hq] (natural log).  A token that sees no key gets O = 0, lse = -inf.
+ * What pages hold behind the last cached token does not matter.  An infinity or NaN in a value row of the cache reaches the tokens
+ * that see it and may reach earlier tokens of the same chunk too.
+ */
+seka_status seka_paged_attention(const seka_paged_shape* shape, const void* Q, const void* K_pages, const void* V_pages,
+                                 void* O, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Accumulated attention weight of the cached rows: with lse as seka_paged_attention gave it for the same queries and cache,
+ *     mass_out[b, h, j] = (j < cache_lens[b] - n_b ? mass_in[b, h, j] : 0) + sum over the new tokens i that see j and the query
+ *                         heads hq of KV head h of exp(Q[t, hq, :] . K[j, h, :] * scale - lse[t, hq])
+ * for j < cache_lens[b] (new rows begin at zero).  fp32, summed in a fixed order.  mass_in == NULL: zeros; mass_out may be mass_in.
+ */
+seka_status seka_attention_mass(const seka_paged_shape* shape, const void* Q, const void* K_pages, const float* lse,
+                                const float* mass_in, float* mass_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Cuts every sequence of more than `keep` cached rows to `keep`, per KV head.  The rows that stay come first in this order: rows
+ * whose position is at least next_pos[b] - recent; then rows whose position p has protect[b * protect_len + p] set (the
+ * highlighted tokens of the prompt; positions outside 0 .. protect_len - 1 are not protected; protect may be NULL); then the
+ * others; each of the three by weight, largest first (a NaN comes last), equal weights by row, lowest first.  Kept rows below `keep` stay
+ * where they are; the freed ones, in ascending order, take K, V, weight and position of the kept rows behind, in ascending order
+ * (attention does not depend on the order of rows).  Rows from `keep` on are left as they were: their pages are free once they
+ * lie wholly behind.
+ *   mass_in, mass_out, pos_in, pos_out   [B, Hkv, cap] fp32 / int32; _out may be _in; the first min(cache_lens[b], keep) rows are written
+ *   next_pos   int32 [B]: positions handed out so far;   lens_out   int32 [B]: min(cache_lens[b], keep), may be cache_lens
+ * Uses batch, heads, head_dim, pages, block_table and cache_lens of the shape.
+ */
+seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_pages, void* V_pages, const float* mass_in, float* mass_out,
+                             const int32_t* pos_in, int32_t* pos_out, const uint8_t* protect, int32_t protect_len,
+                             const int32_t* next_pos, int32_t keep, int32_t recent, int32_t* lens_out,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * The first 256 bytes of a workspace are its status block (int32 words): word 0 the status, word 1 a code for the

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libseka_b200.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-         "-Xcompiler", "-fPIC", "-shared", "--expt-relaxed-constexpr"]
+         "-Xcompiler", "-fPIC", "-shared", "--expt-relaxed-constexpr", "-t", "0"]
 
 
 def sources():
