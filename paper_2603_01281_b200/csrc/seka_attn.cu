@@ -116,34 +116,6 @@ __host__ __device__ inline SmemPlan smem_plan(const SteerPlan& sp) {
     return s;
 }
 
-// true in exactly one lane of a fully active warp
-__device__ __forceinline__ bool elect_one() {
-    uint32_t pred;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
-    return pred != 0;
-}
-
-template <int N> __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-
-// 4 x 4 transpose among groups of four lanes: unit u (16 bytes) of lane q becomes unit q of lane u
-__device__ __forceinline__ void transpose4(uint4 (&a)[4], int lane) {
-    auto swap = [&](uint4& x, uint4& y, int bit) {       // the lane without `bit` gives y for its partner's x
-        const bool up = (lane & bit) != 0;
-        uint4 send = up ? x : y;
-        send.x = __shfl_xor_sync(0xffffffffu, send.x, bit); send.y = __shfl_xor_sync(0xffffffffu, send.y, bit);
-        send.z = __shfl_xor_sync(0xffffffffu, send.z, bit); send.w = __shfl_xor_sync(0xffffffffu, send.w, bit);
-        if (up) x = send; else y = send;
-    };
-    swap(a[0], a[2], 2); swap(a[1], a[3], 2);
-    swap(a[0], a[1], 1); swap(a[2], a[3], 1);
-}
 // 32 columns of the rows of a warp (lane = row), scaled, to global memory: four lanes write 64 contiguous bytes of a row
 // (a row per lane, 32 pieces of 16 bytes an instruction, took 2000 cycles of the load/store unit per tile).  `row0` points at
 // the columns in the row of lane 0, rows are `pitch` elements apart, `n_rows` of them exist.
@@ -998,13 +970,13 @@ static EncodeTiledFn encode_tiled_fn() {
     return fn;
 }
 
-// bf16 tensor [T, H, d] viewed as (d, H, T); tiles of 64 x 1 x box_rows with the 128-byte swizzle.
-bool make_tile_map(CUtensorMap* m, const void* base, int d, int H, long long T, int box_rows) {
+// bf16 tensor [T, H, d] viewed as (d, H, T); tiles of 64 x box_heads x box_rows with the 128-byte swizzle.
+bool make_tile_map(CUtensorMap* m, const void* base, int d, int H, long long T, int box_rows, int box_heads) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (fn == nullptr) return false;
     cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)H, (cuuint64_t)T};
     cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)H * d * 2};
-    cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
     cuuint32_t estr[3] = {1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,

@@ -498,6 +498,52 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t& hi, uint3
     lo = pack_bf16(x - h.x, y - h.y);
 }
 
+// ---------------------------------------------------------------- warps
+// true in exactly one lane of a fully active warp
+__device__ __forceinline__ bool elect_one() {
+    uint32_t pred;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
+    return pred != 0;
+}
+
+template <int N> __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// 4 x 4 transpose among groups of four lanes: unit u (16 bytes) of lane q becomes unit q of lane u
+__device__ __forceinline__ void transpose4(uint4 (&a)[4], int lane) {
+    auto swap = [&](uint4& x, uint4& y, int bit) {       // the lane without `bit` gives y for its partner's x
+        const bool up = (lane & bit) != 0;
+        uint4 send = up ? x : y;
+        send.x = __shfl_xor_sync(0xffffffffu, send.x, bit); send.y = __shfl_xor_sync(0xffffffffu, send.y, bit);
+        send.z = __shfl_xor_sync(0xffffffffu, send.z, bit); send.w = __shfl_xor_sync(0xffffffffu, send.w, bit);
+        if (up) x = send; else y = send;
+    };
+    swap(a[0], a[2], 2); swap(a[1], a[3], 2);
+    swap(a[0], a[1], 1); swap(a[2], a[3], 1);
+}
+
+// ---------------------------------------------------------------- mma.sync (few query rows)
+__device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_x4_trans(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
+}
+// D[16 x 8] += A[16 x 16] B[16 x 8], bf16 operands, fp32 accumulation
+__device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
 #endif  // __CUDACC__
 
 }  // namespace seka

@@ -9,6 +9,7 @@ namespace seka {
 seka_status validate_paged(const seka_paged_shape* s) {
     if (s == nullptr) return SEKA_ERR_INVALID_ARG;
     if (s->batch < 0 || s->total_new < 0 || s->max_new < 0 || s->n_pages < 0 || s->max_pages < 0) return SEKA_ERR_INVALID_ARG;
+    if (s->batch > 0 && (s->n_pages < 1 || s->max_pages < 1)) return SEKA_ERR_INVALID_ARG;
     if (s->n_q_heads <= 0 || s->n_kv_heads <= 0 || s->n_q_heads % s->n_kv_heads != 0) return SEKA_ERR_INVALID_ARG;
     if (s->dtype != SEKA_F32 && s->dtype != SEKA_BF16) return SEKA_ERR_INVALID_ARG;
     if (!(s->softmax_scale >= 0.f) || isinf(s->softmax_scale)) return SEKA_ERR_INVALID_ARG;

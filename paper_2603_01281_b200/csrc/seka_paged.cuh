@@ -37,10 +37,24 @@ SEKA_HD long long pool_row(const PagedView& v, int page, int j) {
 }
 SEKA_HD int table_entry(const PagedView& v, int b, int j) { return v.table[(long long)b * v.max_pages + (j >> v.page_shift)]; }
 
+// Attention: up to this many rows (new tokens x query heads of a KV head) of a sequence the few-row kernel runs, else the tile kernel.
+constexpr int kFewRows = 16;
+static inline bool few_rows(const seka_paged_shape* s) {
+    return (long long)s->max_new * (s->n_q_heads / s->n_kv_heads) <= kFewRows;
+}
+// Shares of a launch (one per CTA: one CTA per SM in the tile kernel, two or three in the few-row kernel) and rows of a unit.  148 SMs;
+// a device with fewer runs the same shares in more than one wave.
+constexpr int kShareSms = 148;
+static inline int attention_shares(const seka_paged_shape* s) { return few_rows(s) ? kShareSms * (s->head_dim == 128 ? 2 : 3) : kShareSms; }
+static inline int unit_rows(const seka_paged_shape* s) { return few_rows(s) ? kFewRows : 256; }
+
 // Workspace of the paged calls (one at a time): status block, then the lists of the eviction or the partial results of the attention.
 struct PagedLayout {
     size_t evict_count_off;     // int32 [B, Hkv]: rows that move
     size_t evict_list_off;      // int32 [B, Hkv, cap]: freed rows from the front, rows that take their place from the back
+    size_t cut_off;             // CutRecord [shares]
+    size_t part_ml_off;         // fp32 [shares, 2, rows, 2]: running maximum (log2 domain) and sum of the cut units of each share
+    size_t part_o_off;          // fp32 [shares, 2, rows, d]: their outputs, not normalised
     size_t total;
 };
 static inline PagedLayout paged_layout(const seka_paged_shape* s) {
@@ -48,7 +62,13 @@ static inline PagedLayout paged_layout(const seka_paged_shape* s) {
     const size_t pairs = (size_t)s->batch * s->n_kv_heads, cap = (size_t)s->max_pages * s->page_size;
     w.evict_count_off = 1024;
     w.evict_list_off = w.evict_count_off + align_up(pairs * 4 + 4, 256);
-    w.total = w.evict_list_off + align_up(pairs * cap * 4 + 4, 256);
+    const size_t evict = w.evict_list_off + align_up(pairs * cap * 4 + 4, 256);
+    const size_t shares = (size_t)attention_shares(s), rows = (size_t)unit_rows(s);
+    w.cut_off = 1024;
+    w.part_ml_off = w.cut_off + align_up(shares * 32, 256);
+    w.part_o_off = w.part_ml_off + shares * 2 * rows * 2 * 4;
+    const size_t attend = w.part_o_off + shares * 2 * rows * s->head_dim * 4;
+    w.total = evict > attend ? evict : attend;
     return w;
 }
 

@@ -1,64 +1,358 @@
-// Attention of new tokens over a paged cache.
+// Attention of new tokens over a paged cache: few rows (single tokens, a few tokens of a small group), and the merge of cut units.
+//
+//   paged_few_kernel      up to 16 rows (new tokens x query heads of a KV head) per unit: bound by HBM, every cached key and value is
+//                         read once.  A producer warp streams 64-token stages of K and V through a ring in shared memory, a TMA box
+//                         per page piece, its lanes issuing side by side; four consumer warps take 16 tokens of each stage, form
+//                         the scores of all rows with mma.sync m16n8k16 (16 rows are too few for a tcgen05 tile), keep
+//                         a private online softmax and P V in registers.  The CTA walks its equal share of all stages, unit after
+//                         unit, without the ring running dry between them.
+//   paged_merge_kernel    merges the parts of a unit that a share boundary cut, a warp per row.
+// Weights are rounded to bf16 for P V (half a step, 2^-8 of each); scores, sums and outputs stay in fp32 until the store.
 #include <math.h>
 
-#include "seka_kernels.h"
-#include "seka_paged.cuh"
+#include "seka_paged_attn.cuh"
 
 namespace seka {
 namespace {
 
-constexpr int PA_WARPS = 4;
+constexpr int FEW_KEYS = 64;                            // cached tokens of a stage
+constexpr int FEW_CONSUMERS = 4, FEW_THREADS = (FEW_CONSUMERS + 1) * 32;
 
-struct PagedAttnParams {
-    PagedView v;
-    const __nv_bfloat16 *Q, *K, *V;
-    __nv_bfloat16* O;
-    float* lse;
-    float scale_log2;
+template <int D>
+struct FewSmem {
+    static constexpr int NSTAGE = D == 128 ? 3 : 4;
+    static constexpr int CTAS_PER_SM = D == 128 ? 2 : 3;
+    static constexpr int TILE_BYTES = FEW_KEYS * D * 2;
+    static constexpr int BLOCK_BYTES = FEW_KEYS * 128;              // one [64 tokens x 64 elements] swizzled block
+    static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
+    static constexpr int MERGE_STRIDE = D + 2;                      // floats of a row: o[D], m, l
+    static constexpr int MERGE_OFF = NSTAGE * STAGE_BYTES;          // [4 warps][8 rows]
+    static constexpr int BAR_OFF = MERGE_OFF + FEW_CONSUMERS * 8 * MERGE_STRIDE * 4;
+    static constexpr int WALK_OFF = BAR_OFF + 2 * NSTAGE * 8;
+    static constexpr int SCRATCH_OFF = WALK_OFF + (FEW_CONSUMERS + 1) * 48;
+    static constexpr int BYTES = SCRATCH_OFF + (FEW_THREADS / 32 + 4) * 8 + 16;
+    static_assert(BAR_OFF % 8 == 0 && WALK_OFF % 16 == 0 && SCRATCH_OFF % 8 == 0, "alignment");
+    static_assert(CTAS_PER_SM * (BYTES + 1024) <= 228 * 1024, "resident CTAs");
 };
 
-// A warp per (token, query head), a key at a time.
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// ... and the same answer for all of them: has any given up?
+__device__ __forceinline__ bool consumer_sync_or(bool x) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(x ? 1u : 0u) : "memory");
+    return r != 0;
+}
+
+// HALF: at most 8 rows, so rows 8..15 of every MMA are padding and their softmax is skipped.
+template <int D, bool HALF>
+__global__ void __launch_bounds__(FEW_THREADS, FewSmem<D>::CTAS_PER_SM)
+paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ PagedAttnParams p) {
+    using SL = FewSmem<D>;
+    constexpr int H = D / 64;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + SL::BAR_OFF);
+    uint64_t* empty = full + SL::NSTAGE;
+    long long* scratch = reinterpret_cast<long long*>(smem + SL::SCRATCH_OFF);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SL::BYTES - 16);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < SL::NSTAGE; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], FEW_CONSUMERS); }
+        *abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_desc(&tk);
+        tma_prefetch_desc(&tv);
+    }
+    pdl_wait();
+    pdl_release();
+    const int status0 = *reinterpret_cast<volatile int*>(p.v.status);
+    if (__syncthreads_or(status0 != 0)) return;             // an earlier launch gave up on this workspace
+    const Share share = find_share<FEW_THREADS>(p.v, p.geo, p.n_shares, (int)blockIdx.x, scratch);
+    if (tid == 0) write_cut(p, share, (int)blockIdx.x);
+    if (share.len == 0) return;
+    Walk* walk = reinterpret_cast<Walk*>(smem + SL::WALK_OFF + warp * 48);
+    if (lane == 0) walk_begin(p.v, share, *walk);
+    __syncwarp();
+    auto next = [&](Segment& s) -> bool {
+        Walk w = *walk;
+        __syncwarp();
+        const bool ok = walk_next(p.v, p.geo, w, s);
+        if (lane == 0) *walk = w;
+        __syncwarp();
+        return ok;
+    };
+    Segment sg;
+
+    if (warp == FEW_CONSUMERS) {
+        // ------------------------------------------------ producer: a lane per TMA box (K or V, 64 columns, a piece of a page)
+        const int bx_shift = p.v.page_shift < 6 ? p.v.page_shift : 6, nb = FEW_KEYS >> bx_shift;
+        const int box = lane % nb, blk = (lane / nb) % H, kv = lane / (nb * H);
+        const uint32_t dst = (uint32_t)(kv * SL::TILE_BYTES + blk * SL::BLOCK_BYTES + (box << bx_shift) * 128);
+        const int pool_rows = p.v.n_pages << p.v.page_shift;
+        // pool row of this lane's box of stage j; -1: it lies behind the cache.  A page that does not exist reads as zeros.
+        auto row_of = [&](int j) -> int {
+            const int key = j * FEW_KEYS + (box << bx_shift);
+            if (key >= sg.L) return -1;
+            const long long r = load_pool_row(p.v, sg.b, key);
+            return r < 0 ? pool_rows : (int)r;
+        };
+        int i = 0;
+        bool ok = true;
+        while (ok && next(sg)) {
+            int row = row_of(sg.j);
+#pragma unroll 1
+            for (int t = 0; t < sg.n; ++t, ++i) {
+                const int s = i % SL::NSTAGE, round = i / SL::NSTAGE;
+                const int row_next = t + 1 < sg.n ? row_of(sg.j + t + 1) : -1;
+                if (round > 0) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&empty[s], (uint32_t)(round - 1) & 1u, abort_flag, p.v.status, 60));
+                    if (!ok) break;
+                }
+                if (lane == 0) {
+                    const int keys = sg.L - (sg.j + t) * FEW_KEYS;
+                    const int n_box = keys <= 0 ? 0 : min(nb, (keys + (1 << bx_shift) - 1) >> bx_shift);
+                    mbar_expect_tx(&full[s], (uint32_t)(2 * H * n_box * 128) << bx_shift);
+                }
+                __syncwarp();
+                if (row >= 0 && kv < 2) tma_load_3d(smem + s * SL::STAGE_BYTES + dst, kv ? &tv : &tk, &full[s], blk * 64, sg.h, row);
+                row = row_next;
+            }
+        }
+        __syncwarp();
+        if (lane == 0 && (!ok || *abort_flag)) {
+            // a wait ran out somewhere: let the copies already issued land before the CTA's shared memory is released
+            for (int k = i > SL::NSTAGE ? i - SL::NSTAGE : 0; k < i; ++k) {
+                const uint64_t t0 = global_timer_ns();
+                while (!mbar_try_wait(&full[k % SL::NSTAGE], (uint32_t)(k / SL::NSTAGE) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) { }
+            }
+        }
+        return;
+    }
+
+    // ---------------------------------------------------- consumers
+    const int G = p.v.G, Hq = p.v.Hq;
+    const int r0 = lane >> 2, cq = (lane & 3) * 2;          // accumulator rows r0 and r0 + 8, columns cq, cq + 1
+    const int tok0 = r0 / G, tok1 = (r0 + 8) / G;           // new token of these rows
+    // ldmatrix source rows of this lane inside the warp's 16 tokens of a stage
+    const int key_k = 16 * warp + (lane & 7) + ((lane >> 4) << 3);         // K: matrices 2, 3 hold tokens 8..15
+    const int key_v = 16 * warp + (lane & 7) + (((lane >> 3) & 1) << 3);   // V: matrices 1, 3 hold tokens 8..15
+    const uint32_t k_row = (uint32_t)key_k * 128u, v_row = (uint32_t)key_v * 128u;
+    const uint32_t k_sel = (uint32_t)((lane >> 3) & 1), v_sel = (uint32_t)(lane >> 4);
+    const uint32_t smem_base = smem_u32(smem);
+    float* mg = reinterpret_cast<float*>(smem + SL::MERGE_OFF);
+    int i = 0;
+    bool ok = true;
+    while (ok && next(sg)) {
+        const int rows = sg.n_new * G;
+        uint32_t qa[D / 16][4];
+        {
+            const __nv_bfloat16* q0 = p.Q + ((size_t)(sg.q0 + tok0) * Hq + (size_t)sg.h * G + (r0 - tok0 * G)) * D;
+            const __nv_bfloat16* q1 = p.Q + ((size_t)(sg.q0 + tok1) * Hq + (size_t)sg.h * G + (r0 + 8 - tok1 * G)) * D;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const int c = kk * 16 + cq;
+                qa[kk][0] = r0 < rows ? *reinterpret_cast<const uint32_t*>(q0 + c) : 0u;
+                qa[kk][2] = r0 < rows ? *reinterpret_cast<const uint32_t*>(q0 + c + 8) : 0u;
+                qa[kk][1] = !HALF && r0 + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + c) : 0u;
+                qa[kk][3] = !HALF && r0 + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + c + 8) : 0u;
+            }
+        }
+        // last cached token that a row sees (padding rows: the last one)
+        const int lim0 = r0 < rows ? sg.old + tok0 : sg.L - 1, lim1 = r0 + 8 < rows ? sg.old + tok1 : sg.L - 1;
+        float o[D / 8][4];
+        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f; }
+#pragma unroll 1
+        for (int t = 0; t < sg.n; ++t, ++i) {
+            const int s = i % SL::NSTAGE;
+            ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(i / SL::NSTAGE) & 1u, abort_flag, p.v.status, 61));
+            if (!ok) break;
+            const uint32_t kt = smem_base + (uint32_t)(s * SL::STAGE_BYTES), vt = kt + SL::TILE_BYTES;
+            // scores of the rows against the warp's 16 tokens: two 16 x 8 tiles
+            float sc[2][4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) { sc[x][0] = sc[x][1] = sc[x][2] = sc[x][3] = 0.f; }
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t chunk = (uint32_t)((kk & 3) * 2) + k_sel;
+                uint32_t b0, b1, b2, b3;
+                ldsm_x4(kt + (uint32_t)((kk >> 2) * SL::BLOCK_BYTES) + k_row + (((chunk ^ (uint32_t)key_k) & 7u) << 4), b0, b1, b2, b3);
+                mma_16816(sc[0], qa[kk], b0, b1);
+                mma_16816(sc[1], qa[kk], b2, b3);
+            }
+            const int base = (sg.j + t) * FEW_KEYS + 16 * warp;
+            if (base + 15 > sg.old) {                       // some row does not see all of the warp's tokens
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (base + 8 * x + cq + (e & 1) > (e < 2 ? lim0 : lim1)) sc[x][e] = -INFINITY;
+                if (base + 16 > sg.L) {                     // values behind the cache may be anything, NaN too
+                    for (int u = lane; u < 16 * H * 8; u += 32) {
+                        const int row = u / (H * 8), c = u % (H * 8);
+                        if (base + row >= sg.L)
+                            *reinterpret_cast<uint4*>(smem + s * SL::STAGE_BYTES + SL::TILE_BYTES + (c >> 3) * SL::BLOCK_BYTES +
+                                                      (16 * warp + row) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    __syncwarp();
+                }
+            }
+            // online softmax, private to the warp; the row sums stay per thread until the end
+            float mx0 = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
+            const float mn0 = fmaxf(m0, mx0 * p.scale_log2);
+            const float ms0 = mn0 == -INFINITY ? 0.f : mn0;
+            const float f0 = fast_exp2(m0 - ms0);
+            float mn1 = -INFINITY, ms1 = 0.f, f1 = 1.f;
+            if (!HALF) {
+                float mx1 = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]));
+                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
+                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
+                mn1 = fmaxf(m1, mx1 * p.scale_log2);
+                ms1 = mn1 == -INFINITY ? 0.f : mn1;
+                f1 = fast_exp2(m1 - ms1);
+            }
+            const bool moved = (mn0 != m0) || (!HALF && mn1 != m1);
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) {
+                    o[j][0] *= f0; o[j][1] *= f0;
+                    if (!HALF) { o[j][2] *= f1; o[j][3] *= f1; }
+                }
+            }
+            m0 = mn0; m1 = mn1;
+            uint32_t pa[4];
+            {
+                const float p00 = fast_exp2(fmaf(sc[0][0], p.scale_log2, -ms0)), p01 = fast_exp2(fmaf(sc[0][1], p.scale_log2, -ms0));
+                const float p10 = fast_exp2(fmaf(sc[1][0], p.scale_log2, -ms0)), p11 = fast_exp2(fmaf(sc[1][1], p.scale_log2, -ms0));
+                l0 = fmaf(l0, f0, (p00 + p01) + (p10 + p11));
+                pa[0] = pack_bf16(p00, p01); pa[2] = pack_bf16(p10, p11);
+                if (!HALF) {
+                    const float q00 = fast_exp2(fmaf(sc[0][2], p.scale_log2, -ms1)), q01 = fast_exp2(fmaf(sc[0][3], p.scale_log2, -ms1));
+                    const float q10 = fast_exp2(fmaf(sc[1][2], p.scale_log2, -ms1)), q11 = fast_exp2(fmaf(sc[1][3], p.scale_log2, -ms1));
+                    l1 = fmaf(l1, f1, (q00 + q01) + (q10 + q11));
+                    pa[1] = pack_bf16(q00, q01); pa[3] = pack_bf16(q10, q11);
+                } else {
+                    pa[1] = 0u; pa[3] = 0u;
+                }
+            }
+            // o[16 x D] += P[16 x 16 tokens] V[16 tokens x D]
+#pragma unroll
+            for (int jp = 0; jp < D / 16; ++jp) {
+                const uint32_t chunk = (uint32_t)((jp & 3) * 2) + v_sel;
+                uint32_t b0, b1, b2, b3;
+                ldsm_x4_trans(vt + (uint32_t)((jp >> 2) * SL::BLOCK_BYTES) + v_row + (((chunk ^ (uint32_t)key_v) & 7u) << 4), b0, b1, b2, b3);
+                mma_16816(o[2 * jp], pa, b0, b1);
+                mma_16816(o[2 * jp + 1], pa, b2, b3);
+            }
+            fence_proxy_async();            // the reads (and zeros) of this stage come before the copies that refill it
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[s]);
+        }
+        // ------------------------------------------------ merge the four warps' states, eight rows at a time
+        l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
+        l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
+        if (!HALF) {
+            l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+        }
+        const size_t slot = (size_t)blockIdx.x * 2 + (sg.first ? 0 : 1);
+#pragma unroll
+        for (int half = 0; half < (HALF ? 1 : 2); ++half) {
+            if (half * 8 >= rows) break;
+            ok = !consumer_sync_or(!ok || *abort_flag != 0);        // the area is free (its last readers are through)
+            if (!ok) break;
+            float* row = mg + ((size_t)warp * 8 + r0) * SL::MERGE_STRIDE;
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(row + 8 * j + cq) = half ? make_float2(o[j][2], o[j][3]) : make_float2(o[j][0], o[j][1]);
+            if ((lane & 3) == 0) { row[D] = half ? m1 : m0; row[D + 1] = half ? l1 : l0; }
+            consumer_sync();
+            const int n = min(8, rows - half * 8);
+            for (int idx = tid; idx < n * D; idx += FEW_CONSUMERS * 32) {
+                const int r = idx / D, c = idx - r * D, ur = half * 8 + r;
+                float mw[FEW_CONSUMERS], M = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < FEW_CONSUMERS; ++w) { mw[w] = mg[((size_t)w * 8 + r) * SL::MERGE_STRIDE + D]; M = fmaxf(M, mw[w]); }
+                float acc = 0.f, lsum = 0.f;
+#pragma unroll
+                for (int w = 0; w < FEW_CONSUMERS; ++w) {
+                    const float f = mw[w] == -INFINITY ? 0.f : fast_exp2(mw[w] - M);
+                    acc = fmaf(mg[((size_t)w * 8 + r) * SL::MERGE_STRIDE + c], f, acc);
+                    lsum = fmaf(mg[((size_t)w * 8 + r) * SL::MERGE_STRIDE + D + 1], f, lsum);
+                }
+                if (sg.whole) {
+                    const int tok = ur / G;
+                    const size_t out = (size_t)(sg.q0 + tok) * Hq + (size_t)sg.h * G + (ur - tok * G);
+                    p.O[out * D + c] = __float2bfloat16(lsum == 0.f ? 0.f : acc / lsum);
+                    if (p.lse != nullptr && c == 0) p.lse[out] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
+                } else {
+                    p.part_o[(slot * kFewRows + ur) * D + c] = acc;
+                    if (c == 0) *reinterpret_cast<float2*>(p.part_ml + (slot * kFewRows + ur) * 2) = make_float2(M, lsum);
+                }
+            }
+        }
+    }
+}
+
+// A block per (cut, eight rows): nothing to do where the share begins with a unit, or where an earlier cut of the same unit does it.
+constexpr int MERGE_WARPS = 8;
 template <int D>
-__global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAttnParams p) {
+__global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttnParams p, int unit_rows) {
     constexpr int E = D / 32;
+    const int blocks = unit_rows / MERGE_WARPS, cut = (int)blockIdx.x / blocks;
+    const int r = ((int)blockIdx.x - cut * blocks) * MERGE_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     pdl_wait();
     pdl_release();
     if (*p.v.status != 0) return;
-    const long long w = (long long)blockIdx.x * PA_WARPS + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (w >= (long long)p.v.T * p.v.Hq) return;
-    const int t = (int)(w / p.v.Hq), hq = (int)(w % p.v.Hq), h = hq / p.v.G;
-    int b = -1, limit = -1;
-    for (int i = 0; i < p.v.B; ++i) {
-        const int q0 = p.v.cu ? p.v.cu[i] : i * p.v.max_new, q1 = p.v.cu ? p.v.cu[i + 1] : q0 + p.v.max_new;
-        if (t >= q0 && t < q1) {
-            const PagedSeq s = load_seq(p.v, i);
-            if (s.valid) { b = i; limit = s.L - s.n + (t - q0); }
+    const CutRecord c = p.cuts[cut];
+    if (c.n == 0 || c.j == 0 || c.j > c.share) return;
+    // row -> new token and query head
+    const int tile = r >> 7, rt = r & 127, t_tile = rt / p.v.G, tok = c.p * p.geo.tp + tile * p.tile_tokens + t_tile;
+    const PagedSeq s = paged_seq(p.v, c.b);
+    if (t_tile >= p.tile_tokens || tok >= s.n) return;
+    const size_t out = (size_t)(s.q0 + tok) * p.v.Hq + (size_t)c.h * p.v.G + (rt - t_tile * p.v.G);
+    // parts: the last segment of share cut - 1, then the first ones of the shares on
+    const int parts = 1 + (c.n - c.j + c.share - 1) / c.share;
+    auto slot = [&](int i) -> size_t { return i == 0 ? (size_t)(cut - 1) * 2 + (c.j < c.share ? 1 : 0) : (size_t)(cut - 1 + i) * 2; };
+    float M = -INFINITY, l = 0.f, acc[E] = {};
+    for (int i0 = 0; i0 < parts; i0 += 32) {
+        const int n = min(32, parts - i0);
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < n) ml = *reinterpret_cast<const float2*>(p.part_ml + (slot(i0 + lane) * unit_rows + r) * 2);
+        float mx = fmaxf(M, ml.x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float keep = M == -INFINITY ? 0.f : fast_exp2(M - mx), f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - mx);
+        l = fmaf(l, keep, ml.y * f);                        // per lane until the end
+        M = mx;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] *= keep;
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) {
+            const float fi = __shfl_sync(0xffffffffu, f, i);
+            const float* src = p.part_o + (slot(i0 + i) * unit_rows + r) * D + lane * E;
+            float x[E];
+            if (E == 4) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(src);
+            else *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(src);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(x[e], fi, acc[e]);
         }
     }
-    float q[E], o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) { q[e] = __bfloat162float(p.Q[(size_t)w * D + lane + 32 * e]); o[e] = 0.f; }
-    for (int j = 0; j <= limit; ++j) {
-        const long long row = load_pool_row(p.v, b, j);
-        if (row < 0) break;
-        const __nv_bfloat16 *k = p.K + ((size_t)row * p.v.Hkv + h) * D, *v = p.V + ((size_t)row * p.v.Hkv + h) * D;
-        float s = 0.f;
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(p.O + out * D + lane * E);
 #pragma unroll
-        for (int e = 0; e < E; ++e) s = fmaf(q[e], __bfloat162float(k[lane + 32 * e]), s);
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-        s *= p.scale_log2;
-        const float mn = fmaxf(m, s), f = mn == -INFINITY ? 1.f : exp2f(m - mn), pe = mn == -INFINITY ? 0.f : exp2f(s - mn);
-        l = l * f + pe;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + pe * __bfloat162float(v[lane + 32 * e]);
-        m = mn;
-    }
-    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-#pragma unroll
-    for (int e = 0; e < E; ++e) p.O[(size_t)w * D + lane + 32 * e] = __float2bfloat16(o[e] * inv);
-    if (p.lse != nullptr && lane == 0) p.lse[w] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+    for (int e = 0; e < E / 2; ++e) dst[e] = pack_bf16(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    if (p.lse != nullptr && lane == 0) p.lse[out] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
+}
+
+template <int D, bool HALF>
+seka_status launch_few(const CUtensorMap& tk, const CUtensorMap& tv, const PagedAttnParams& p, unsigned grid, cudaStream_t st) {
+    using SL = FewSmem<D>;
+    if (cudaFuncSetAttribute(paged_few_kernel<D, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, SL::BYTES) != cudaSuccess) return SEKA_ERR_CUDA;
+    return launch_kernel(true, paged_few_kernel<D, HALF>, grid, FEW_THREADS, SL::BYTES, st, tk, tv, p);
 }
 
 }  // namespace
@@ -70,19 +364,49 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     seka_status stc = validate_paged(shape);
     if (stc != SEKA_OK) return stc;
     if (shape->batch == 0 || shape->total_new == 0) return SEKA_OK;
-    if (!Q || !O || ((!K_pages || !V_pages) && shape->n_pages > 0)) return SEKA_ERR_INVALID_ARG;
+    if (!Q || !O || !K_pages || !V_pages) return SEKA_ERR_INVALID_ARG;
     if (((uintptr_t)Q | (uintptr_t)K_pages | (uintptr_t)V_pages | (uintptr_t)O) & 15) return SEKA_ERR_INVALID_ARG;
     stc = check_paged_call(shape, workspace, workspace_bytes);
     if (stc != SEKA_OK) return stc;
+    const PagedLayout w = paged_layout(shape);
+    char* ws = static_cast<char*>(workspace);
+    const int D = shape->head_dim, G = shape->n_q_heads / shape->n_kv_heads;
+    const bool few = few_rows(shape);
     PagedAttnParams p;
     p.v = paged_view(shape, workspace);
-    p.Q = static_cast<const __nv_bfloat16*>(Q); p.K = static_cast<const __nv_bfloat16*>(K_pages); p.V = static_cast<const __nv_bfloat16*>(V_pages);
-    p.O = static_cast<__nv_bfloat16*>(O); p.lse = lse;
-    const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / sqrtf((float)shape->head_dim);
+    p.Q = static_cast<const __nv_bfloat16*>(Q); p.O = static_cast<__nv_bfloat16*>(O); p.lse = lse;
+    const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / sqrtf((float)D);
     p.scale_log2 = scale * 1.4426950408889634f;
-    const long long warps = (long long)shape->total_new * shape->n_q_heads;
-    const unsigned grid = (unsigned)((warps + PA_WARPS - 1) / PA_WARPS);
+    p.tile_tokens = few ? shape->max_new : 128 / G;
+    p.geo.tp = few ? shape->max_new : 2 * p.tile_tokens;
+    p.geo.shift = few ? 6 : 7;
+    p.geo.min_share = 4;
+    // shares that can have a step, from what the host knows
+    const long long units = few ? shape->batch : (long long)shape->total_new / p.geo.tp + shape->batch;
+    const long long steps = units * shape->n_kv_heads * ((p.v.cap + (1 << p.geo.shift) - 1) >> p.geo.shift);
+    long long shares = (steps + p.geo.min_share - 1) / p.geo.min_share;
+    if (shares > attention_shares(shape)) shares = attention_shares(shape);
+    p.n_shares = (int)shares;
+    p.cuts = reinterpret_cast<CutRecord*>(ws + w.cut_off);
+    p.part_ml = reinterpret_cast<float*>(ws + w.part_ml_off);
+    p.part_o = reinterpret_cast<float*>(ws + w.part_o_off);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return shape->head_dim == 128 ? launch_kernel(true, paged_attn_kernel<128>, grid, PA_WARPS * 32, 0, st, p)
-                                  : launch_kernel(true, paged_attn_kernel<64>, grid, PA_WARPS * 32, 0, st, p);
+    if (few) {
+        const int box = shape->page_size < FEW_KEYS ? shape->page_size : FEW_KEYS;
+        const long long rows = (long long)shape->n_pages * shape->page_size;
+        CUtensorMap tk, tv;
+        if (!make_tile_map(&tk, K_pages, D, shape->n_kv_heads, rows, box) || !make_tile_map(&tv, V_pages, D, shape->n_kv_heads, rows, box)) return SEKA_ERR_CUDA;
+        const bool half = shape->max_new * G <= 8;
+        const unsigned grid = (unsigned)p.n_shares;
+        stc = D == 128 ? (half ? launch_few<128, true>(tk, tv, p, grid, st) : launch_few<128, false>(tk, tv, p, grid, st))
+                       : (half ? launch_few<64, true>(tk, tv, p, grid, st) : launch_few<64, false>(tk, tv, p, grid, st));
+    } else {
+        stc = D == 128 ? launch_paged_tiles<128>(p, Q, K_pages, V_pages, shape->page_size, st)
+                       : launch_paged_tiles<64>(p, Q, K_pages, V_pages, shape->page_size, st);
+    }
+    if (stc != SEKA_OK || p.n_shares == 1) return stc;
+    const int rows = unit_rows(shape);
+    const unsigned grid = (unsigned)(p.n_shares * (rows / MERGE_WARPS));
+    return D == 128 ? launch_kernel(true, paged_merge_kernel<128>, grid, MERGE_WARPS * 32, 0, st, p, rows)
+                    : launch_kernel(true, paged_merge_kernel<64>, grid, MERGE_WARPS * 32, 0, st, p, rows);
 }

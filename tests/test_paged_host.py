@@ -169,3 +169,50 @@ def test_device_checks_on_the_host(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-I", build.CSRC, "-I", cuda, str(src), "-o", str(exe)], check=True)
     out = subprocess.run([str(exe)], capture_output=True, text=True)
     assert out.returncode == 0, out.stdout
+
+
+SCHED = r'''
+#include <stdio.h>
+#include <stdlib.h>
+#include "seka_paged_sched.cuh"
+using namespace seka;
+int main() {
+    unsigned seed = 12345;
+    auto rnd = [&](int lo, int hi) { seed = seed * 1664525u + 1013904223u; return lo + (int)((seed >> 8) % (unsigned)(hi - lo + 1)); };
+    int bad = 0;
+    auto expect = [&](bool ok, int line) { if (!ok && bad++ < 5) printf("line %d\n", line); };
+    for (int rep = 0; rep < 3000; ++rep) {
+        StepGeo g;
+        g.shift = rnd(6, 7); g.tp = rep % 3 == 0 ? rnd(1, 9) : rep % 3 == 1 ? 256 / rnd(1, 128) : rnd(1, 4096); g.min_share = 1;
+        if (g.tp < 1) g.tp = 1;
+        const int n = rnd(1, rep % 2 ? 40 : 3000), L = rep % 5 == 0 ? rnd(0, n + 100) : n + rnd(0, 9000), U = seq_units(g, n);
+        long long s = 0;
+        for (int u = 0; u <= U; ++u) {
+            expect(head_steps(g, L, n, u) == s, __LINE__);
+            if (u == U) break;
+            const int last = (u + 1) * g.tp < n ? (u + 1) * g.tp : n, keys = L - n + last, K = 1 << g.shift;
+            const int want = keys <= 0 ? 1 : (keys + K - 1) / K;
+            expect(unit_steps(g, L, n, u) == want, __LINE__);
+            const int h = rnd(0, 3);
+            const long long per = head_steps(g, L, n, U);
+            for (int j : {0, want / 2, want - 1}) {
+                const LinePos c = place_in_seq(g, 7, L, n, per, h * per + s + j);
+                expect(c.b == 7 && c.h == h && c.p == u && c.j == j, __LINE__);
+            }
+            s += want;
+        }
+    }
+    StepGeo g = {1, 7, 1};          // the longest cache
+    expect(unit_steps(g, 0x7fff0000, 1, 0) == 0x7fff0000 / 128, __LINE__);
+    return bad ? 1 : 0;
+}
+'''
+
+
+def test_division_among_ctas_on_the_host(tmp_path):
+    src, exe = tmp_path / "sched.cpp", tmp_path / "sched"
+    src.write_text(SCHED)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(build.NVCC)), "include")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", build.CSRC, "-I", cuda, str(src), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
