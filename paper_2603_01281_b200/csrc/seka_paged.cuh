@@ -48,13 +48,15 @@ constexpr int kShareSms = 148;
 static inline int attention_shares(const seka_paged_shape* s) { return few_rows(s) ? kShareSms * (s->head_dim == 128 ? 2 : 3) : kShareSms; }
 static inline int unit_rows(const seka_paged_shape* s) { return few_rows(s) ? kFewRows : 256; }
 
-// Workspace of the paged calls (one at a time): status block, then the lists of the eviction or the partial results of the attention.
+// Workspace of the paged calls (one at a time): status block, then the lists of the eviction or the partial results of
+// the attention or of the accumulated weights.
 struct PagedLayout {
     size_t evict_count_off;     // int32 [B, Hkv]: rows that move
     size_t evict_list_off;      // int32 [B, Hkv, cap]: freed rows from the front, rows that take their place from the back
     size_t cut_off;             // CutRecord [shares]
     size_t part_ml_off;         // fp32 [shares, 2, rows, 2]: running maximum (log2 domain) and sum of the cut units of each share
     size_t part_o_off;          // fp32 [shares, 2, rows, d]: their outputs, not normalised
+    size_t mass_part_off;       // fp32 [148, 2, 256]: weights of the cut units of each share
     size_t total;
 };
 static inline PagedLayout paged_layout(const seka_paged_shape* s) {
@@ -68,7 +70,10 @@ static inline PagedLayout paged_layout(const seka_paged_shape* s) {
     w.part_ml_off = w.cut_off + align_up(shares * 32, 256);
     w.part_o_off = w.part_ml_off + shares * 2 * rows * 2 * 4;
     const size_t attend = w.part_o_off + shares * 2 * rows * s->head_dim * 4;
+    w.mass_part_off = w.cut_off + align_up((size_t)kShareSms * 32, 256);
+    const size_t mass = w.mass_part_off + (size_t)kShareSms * 2 * 256 * 4;
     w.total = evict > attend ? evict : attend;
+    if (mass > w.total) w.total = mass;
     return w;
 }
 

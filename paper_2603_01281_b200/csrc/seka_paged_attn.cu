@@ -67,7 +67,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
     const int status0 = *reinterpret_cast<volatile int*>(p.v.status);
     if (__syncthreads_or(status0 != 0)) return;             // an earlier launch gave up on this workspace
     const Share share = find_share<FEW_THREADS>(p.v, p.geo, p.n_shares, (int)blockIdx.x, scratch);
-    if (tid == 0) write_cut(p, share, (int)blockIdx.x);
+    if (tid == 0) write_cut(p.cuts, p.v, p.geo, share, (int)blockIdx.x);
     if (share.len == 0) return;
     Walk* walk = reinterpret_cast<Walk*>(smem + SL::WALK_OFF + warp * 48);
     if (lane == 0) walk_begin(p.v, share, *walk);

@@ -23,15 +23,4 @@ struct PagedAttnParams {
 // many rows: tcgen05 tiles
 template <int D> seka_status launch_paged_tiles(const PagedAttnParams& p, const void* Q, const void* K, const void* V, int page_size, cudaStream_t st);
 
-#ifdef __CUDACC__
-__device__ __forceinline__ void write_cut(const PagedAttnParams& p, const Share& s, int cta) {
-    CutRecord c = {s.at.b, s.at.h, s.at.p, s.at.j, 0, s.share};
-    if (s.len > 0) {
-        const PagedSeq q = paged_seq(p.v, s.at.b);
-        c.n = unit_steps(p.geo, q.L, q.n, s.at.p);
-    }
-    p.cuts[cta] = c;
-}
-#endif
-
 }  // namespace seka

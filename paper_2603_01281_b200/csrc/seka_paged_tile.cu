@@ -104,7 +104,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const int status0 = *reinterpret_cast<volatile int*>(p.v.status), hook_skip = p.v.status[4], limit_us = p.v.status[5];
     if (__syncthreads_or(status0 != 0)) return;              // an earlier launch gave up on this workspace
     const Share share = find_share<NTHREADS>(p.v, p.geo, p.n_shares, (int)blockIdx.x, scratch);
-    if (tid == 0) write_cut(p, share, (int)blockIdx.x);
+    if (tid == 0) write_cut(p.cuts, p.v, p.geo, share, (int)blockIdx.x);
     if (share.len == 0) return;
     if (warp == 0) { tmem_alloc(tmem_holder, TMEM_COLS); tmem_relinquish(); }
     Walk* walk = reinterpret_cast<Walk*>(smem + G::WALK_OFF + warp * 48);      // kept in shared memory: no registers between segments
