@@ -1,11 +1,13 @@
 // Eviction: every (sequence, KV head) of more than `keep` cached rows is cut to the `keep` that come first by (class, weight, row).
 //
-//   evict_select_kernel   one CTA per (sequence, KV head).  A row's rank is a number of 34 bits: its class (2: recent, 1: highlighted,
-//                         0) above its weight mapped so that unsigned order is the order of the weights.  The number of the
-//                         keep-th row is found digit by digit (the class, then 11, 11 and 10 bits) from histograms in shared memory;
-//                         a last pass in row order lists the freed rows below `keep` and the kept ones behind, ties by
-//                         row, and writes weights and positions.
-//   evict_move_kernel     copies K and V of the kept rows behind into the freed rows, a warp per row.
+//   evict_select_kernel   a cluster of 1 to 8 CTAs per (sequence, KV head), a run of consecutive rows each.  A row's rank is its class (2:
+//                         recent, 1: highlighted, 0) above its weight mapped to 32 bits whose unsigned order is the order of the
+//                         weights; both are formed once and kept in shared memory (where they fit).  The class that the keep-th row
+//                         belongs to follows from the counts, its weight is found in four digits of eight bits: a CTA's
+//                         histogram has a column per lane (256 x 32 words: a warp's updates never meet), the CTAs add their totals through
+//                         distributed shared memory.  Then ties by row, and the lists of the freed rows below `keep` and the
+//                         kept ones behind, every warp on consecutive rows so that ranks come from ballots.
+//   evict_move_kernel     copies K, V, weight and position of the kept rows behind into the freed rows.
 // What is kept below `keep` does not move: a cache that is cut often, by a little each time, moves only that little.  Sources lie at or
 // behind `keep`, destinations below it, so the copies need no order.
 #include <math.h>
@@ -16,8 +18,9 @@
 namespace seka {
 namespace {
 
-constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32;
-constexpr int EV_BINS = 2048;
+constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
+constexpr int EV_MAX_CLUSTER = 8;
+constexpr int EV_MAX_CACHED = 36 * 1024;                // rows of a CTA whose ranks fit in shared memory beside the histogram
 
 struct EvictParams {
     PagedView v;
@@ -30,6 +33,7 @@ struct EvictParams {
     int protect_len;
     const int* next_pos;
     int keep, recent;
+    int cluster, cached;        // CTAs of a (sequence, KV head) in the first launch; rows whose ranks are kept in shared memory
     int move_blocks;            // blocks of a (sequence, KV head) in the second launch
     int* lens_out;
     int* count;                 // [B, Hkv] rows that move
@@ -43,145 +47,252 @@ SEKA_HD uint32_t mass_order(float x, uint32_t bits) {
     return (bits & 0x80000000u) ? ~bits : bits | 0x80000000u;
 }
 
-__device__ __forceinline__ int block_sum_scan(int x, int* warp_tot, int& total) {      // exclusive scan over the block
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = x;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-    }
-    __syncthreads();                        // warp_tot of the scan before has been read
-    if (lane == 31) warp_tot[warp] = inc;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < EV_WARPS; ++w) {
-        if (w < warp) before += warp_tot[w];
-        total += warp_tot[w];
-    }
-    return before + inc - x;
+struct EvSmem {
+    int hist[256][32];
+    int tot[2][256];            // this CTA's totals of a digit (read by the cluster; two, so that one barrier per digit is enough)
+    int sum[256];
+    int xch[3][4];              // what the CTAs tell each other: class counts and status; ties; freed and late rows
+    int warp_a[EV_WARPS], warp_b[EV_WARPS];
+    int found[2];
+};
+
+__device__ __forceinline__ int ld_cluster(const int* local, int rank) {
+    uint32_t a;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(local)), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictParams p) {
-    __shared__ int hist[EV_BINS];
-    __shared__ int warp_tot[EV_WARPS];
-    __shared__ int found[2];
-    const int b = blockIdx.x / p.v.Hkv, tid = threadIdx.x;
+    extern __shared__ __align__(16) uint8_t smem[];
+    EvSmem& sm = *reinterpret_cast<EvSmem*>(smem);
+    uint32_t* ord_s = reinterpret_cast<uint32_t*>(smem + sizeof(EvSmem));
+    uint8_t* cls_s = reinterpret_cast<uint8_t*>(ord_s + p.cached);
+    const int C = p.cluster, pair = (int)blockIdx.x / C, rank = (int)blockIdx.x - pair * C, b = pair / p.v.Hkv;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const unsigned all = 0xffffffffu, below = (1u << lane) - 1;
     pdl_wait();
     pdl_release();
-    if (*p.v.status != 0) return;
-    int L = p.v.lens[b];
-    if (L < 0 || L > p.v.cap) {
-        if (tid == 0) { report_invalid(p.v.status, kWhereSeq); p.count[blockIdx.x] = 0; }
+    const int status0 = *reinterpret_cast<volatile int*>(p.v.status);
+    const int L = p.v.lens[b], keep = p.keep;
+    if (L < 0 || L > p.v.cap) {                         // (the same for the whole cluster)
+        if (tid == 0 && rank == 0) { report_invalid(p.v.status, kWhereSeq); p.count[pair] = 0; }
         return;
     }
-    const size_t base = (size_t)blockIdx.x * p.v.cap;
+    const size_t base = (size_t)pair * p.v.cap;
     const float* mass = p.mass_in + base;
     const int* pos = p.pos_in + base;
-    const int keep = p.keep;
     if (L <= keep) {
-        for (int j = tid; j < L; j += EV_THREADS) {
-            if (p.mass_out != p.mass_in) p.mass_out[base + j] = mass[j];
-            if (p.pos_out != p.pos_in) p.pos_out[base + j] = pos[j];
-        }
-        if (tid == 0) p.count[blockIdx.x] = 0;
+        if (status0 == 0)
+            for (int j = rank * EV_THREADS + tid; j < L; j += C * EV_THREADS) {
+                if (p.mass_out != p.mass_in) p.mass_out[base + j] = mass[j];
+                if (p.pos_out != p.pos_in) p.pos_out[base + j] = pos[j];
+            }
+        if (tid == 0 && rank == 0) p.count[pair] = 0;
         return;
     }
+    // rows of this CTA [lo, hi), of this warp [wlo, whi): consecutive, multiples of 32
+    const int wrows = ((L + C * EV_WARPS - 1) / (C * EV_WARPS) + 31) & ~31, chunk = wrows * EV_WARPS;
+    const long long lo_l = (long long)rank * chunk;
+    const int lo = (int)(lo_l < L ? lo_l : L), hi = L - lo < chunk ? L : lo + chunk;
+    const int wlo = hi - lo < warp * wrows ? hi : lo + warp * wrows, whi = hi - wlo < wrows ? hi : wlo + wrows;
+    const bool cached = chunk <= p.cached;
     const long long recent_from = (long long)p.next_pos[b] - p.recent;
-    auto klass = [&](int j) -> int {
+    auto rank_of = [&](int j, uint32_t& o) -> int {     // class, and the weight's order
+        const float m = mass[j];
         const int x = pos[j];
+        o = mass_order(m, __float_as_uint(m));
         if ((long long)x >= recent_from) return 2;
         return (p.protect != nullptr && x >= 0 && x < p.protect_len && p.protect[(size_t)b * p.protect_len + x] != 0) ? 1 : 0;
     };
-    auto order = [&](int j) -> uint32_t { const float x = mass[j]; return mass_order(x, __float_as_uint(x)); };
-
-    // digit 0: the class; digits 1 to 3: the weight.  `need` rows are still to be taken among those that agree with the digits so far.
-    int need = keep, cut_class = 0;
+    auto get = [&](int j, uint32_t& o) -> int {
+        if (!cached) return rank_of(j, o);
+        o = ord_s[j - lo];
+        return cls_s[j - lo];
+    };
+    int n2 = 0, n1 = 0;
+#pragma unroll 4
+    for (int j = wlo + lane; j < whi; j += 32) {
+        uint32_t o;
+        const int c = rank_of(j, o);
+        if (cached) { ord_s[j - lo] = o; cls_s[j - lo] = (uint8_t)c; }
+        n2 += c == 2; n1 += c == 1;
+    }
+    n2 = __reduce_add_sync(all, n2); n1 = __reduce_add_sync(all, n1);
+    if (lane == 0) { sm.warp_a[warp] = n2; sm.warp_b[warp] = n1; }
+    __syncthreads();
+    if (tid == 0) {
+        int a = 0, c = 0;
+        for (int w = 0; w < EV_WARPS; ++w) { a += sm.warp_a[w]; c += sm.warp_b[w]; }
+        sm.xch[0][0] = a; sm.xch[0][1] = c; sm.xch[0][2] = status0;
+    }
+    cluster_barrier();
+    n2 = 0; n1 = 0;
+    int bad = 0;
+    for (int r = 0; r < C; ++r) { n2 += ld_cluster(&sm.xch[0][0], r); n1 += ld_cluster(&sm.xch[0][1], r); bad |= ld_cluster(&sm.xch[0][2], r); }
+    if (bad) { cluster_barrier(); return; }             // an earlier launch gave up (decided together: nobody leaves while others read)
+    const int cut_class = n2 >= keep ? 2 : n2 + n1 >= keep ? 1 : 0;
+    // `need` rows are still to be taken among those of the class that agree with the digits so far
+    int need = keep - (cut_class < 2 ? n2 : 0) - (cut_class < 1 ? n1 : 0);
     uint32_t cut = 0;
     for (int digit = 0; digit < 4; ++digit) {
-        const int shift = digit == 1 ? 21 : digit == 2 ? 10 : 0, bins = digit == 0 ? 3 : digit == 3 ? 1024 : 2048;
-        const uint32_t above = digit <= 1 ? 0u : digit == 2 ? 0xffe00000u : 0xfffffc00u;
-        for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
+        const int shift = 24 - 8 * digit;
+        const uint32_t above = digit == 0 ? 0u : 0xffffffffu << (shift + 8);
+        for (int i = tid; i < 256 * 32 / 4; i += EV_THREADS) reinterpret_cast<int4*>(&sm.hist[0][0])[i] = make_int4(0, 0, 0, 0);
         __syncthreads();
-        for (int j = tid; j < L; j += EV_THREADS) {
-            const int c = klass(j);
-            if (digit == 0) { atomicAdd(&hist[c], 1); continue; }
-            if (c != cut_class) continue;
-            const uint32_t o = order(j);
-            if ((o & above) == (cut & above)) atomicAdd(&hist[(o >> shift) & (uint32_t)(bins - 1)], 1);
+#pragma unroll 4
+        for (int j = wlo + lane; j < whi; j += 32) {
+            uint32_t o;
+            const int c = get(j, o);
+            if (c == cut_class && (o & above) == cut) atomicAdd(&sm.hist[(o >> shift) & 255][lane], 1);
         }
         __syncthreads();
-        // the bin, counted from the top, in which the need-th row lies: two bins a thread, highest first
-        int x0 = 0, x1 = 0;
-        const int i0 = EV_BINS - 1 - 2 * tid, i1 = i0 - 1;
-        x0 = hist[i0]; x1 = hist[i1];
-        int total;
-        const int before = block_sum_scan(x0 + x1, warp_tot, total);
-        if (before < need && before + x0 >= need) { found[0] = i0; found[1] = need - before; }
-        else if (before + x0 < need && before + x0 + x1 >= need) { found[0] = i1; found[1] = need - before - x0; }
+        for (int i = warp; i < 256; i += EV_WARPS) {
+            const int x = __reduce_add_sync(all, sm.hist[i][lane]);
+            if (lane == 0) sm.tot[digit & 1][i] = x;
+        }
+        cluster_barrier();
+        if (tid < 256) {
+            int x = 0;
+            for (int r = 0; r < C; ++r) x += ld_cluster(&sm.tot[digit & 1][tid], r);
+            sm.sum[tid] = x;
+        }
         __syncthreads();
-        need = found[1];
-        if (digit == 0) cut_class = found[0];
-        else cut |= (uint32_t)found[0] << shift;
+        // the bin, counted from the top, in which the need-th row lies: eight bins a lane
+        if (warp == 0) {
+            int x[8], t = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { x[i] = sm.sum[255 - 8 * lane - i]; t += x[i]; }
+            int inc = t;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(all, inc, o);
+                if (lane >= o) inc += y;
+            }
+            int before = inc - t;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (before < need && before + x[i] >= need) { sm.found[0] = 255 - 8 * lane - i; sm.found[1] = need - before; }
+                before += x[i];
+            }
+        }
         __syncthreads();
+        cut |= (uint32_t)sm.found[0] << shift;
+        need = sm.found[1];
+        // (found and sum are written again behind the next digit's barriers)
     }
-    // in row order: ties by row, freed rows below `keep` to the front of the list, kept rows behind to its back
-    int* list = p.list + base;
-    int ties = 0, freed = 0, late = 0;
-    for (int j0 = 0; j0 < L; j0 += EV_THREADS) {
-        const int j = j0 + tid;
-        bool in = false, tie = false;
-        if (j < L) {
-            const int c = klass(j);
-            if (c == cut_class) { const uint32_t o = order(j); in = o > cut; tie = o == cut; }
-            else in = c > cut_class;
+    // ties: the first `need` rows, in row order, of those whose rank is the cut's
+    int mine = 0;
+    for (int j = wlo + lane; j - lane < whi; j += 32) {
+        uint32_t o = 0;
+        const bool tie = j < whi && get(j, o) == cut_class && o == cut;
+        mine += __popc(__ballot_sync(all, tie));
+    }
+    if (lane == 0) sm.warp_a[warp] = mine;
+    __syncthreads();
+    if (tid == 0) {
+        int a = 0;
+        for (int w = 0; w < EV_WARPS; ++w) a += sm.warp_a[w];
+        sm.xch[1][0] = a;
+    }
+    cluster_barrier();
+    int ties = 0;
+    for (int r = 0; r < rank; ++r) ties += ld_cluster(&sm.xch[1][0], r);
+    for (int w = 0; w < warp; ++w) ties += sm.warp_a[w];
+    // who is in; `t` counts the ties before the rows of this step
+    auto decide = [&](int j, int& t) -> bool {
+        uint32_t o = 0;
+        int c = -1;
+        if (j < whi) c = get(j, o);
+        const bool tie = c == cut_class && o == cut;
+        const unsigned bal = __ballot_sync(all, tie);
+        const bool in = c > cut_class || (c == cut_class && o > cut) || (tie && t + __popc(bal & below) < need);
+        t += __popc(bal);
+        return in;
+    };
+    int freed = 0, late = 0;
+    {
+        int t = ties;
+        for (int j = wlo + lane; j - lane < whi; j += 32) {
+            const bool in = decide(j, t);
+            freed += __popc(__ballot_sync(all, j < whi && j < keep && !in));
+            late += __popc(__ballot_sync(all, j < whi && j >= keep && in));
         }
-        int total;
-        const int rank = ties + block_sum_scan(tie ? 1 : 0, warp_tot, total);
-        ties += total;
-        if (tie && rank < need) in = true;
-        const bool gone = j < keep && !in, back = j >= keep && j < L && in;
-        const int at_f = freed + block_sum_scan(gone ? 1 : 0, warp_tot, total);
-        freed += total;
-        const int at_b = late + block_sum_scan(back ? 1 : 0, warp_tot, total);
-        late += total;
-        if (gone) list[at_f] = j;
-        if (back) list[p.v.cap - 1 - at_b] = j;
+    }
+    __syncthreads();                                    // warp_a has been read
+    if (lane == 0) { sm.warp_a[warp] = freed; sm.warp_b[warp] = late; }
+    __syncthreads();
+    if (tid == 0) {
+        int a = 0, c = 0;
+        for (int w = 0; w < EV_WARPS; ++w) { a += sm.warp_a[w]; c += sm.warp_b[w]; }
+        sm.xch[2][0] = a; sm.xch[2][1] = c;
+    }
+    cluster_barrier();
+    int at_f = 0, at_l = 0, moved = 0;
+    for (int r = 0; r < C; ++r) {
+        const int a = ld_cluster(&sm.xch[2][0], r), c = ld_cluster(&sm.xch[2][1], r);
+        if (r < rank) { at_f += a; at_l += c; }
+        moved += a;
+    }
+    for (int w = 0; w < warp; ++w) { at_f += sm.warp_a[w]; at_l += sm.warp_b[w]; }
+    int* list = p.list + base;
+    for (int j = wlo + lane; j - lane < whi; j += 32) {
+        const bool in = decide(j, ties), gone = j < whi && j < keep && !in, back = j < whi && j >= keep && in;
+        const unsigned bf = __ballot_sync(all, gone), bl = __ballot_sync(all, back);
+        if (gone) list[at_f + __popc(bf & below)] = j;
+        if (back) list[p.v.cap - 1 - (at_l + __popc(bl & below))] = j;
+        at_f += __popc(bf); at_l += __popc(bl);
         if (j < keep && in) {
             if (p.mass_out != p.mass_in) p.mass_out[base + j] = mass[j];
             if (p.pos_out != p.pos_in) p.pos_out[base + j] = pos[j];
         }
     }
-    __syncthreads();
-    for (int i = tid; i < freed; i += EV_THREADS) {
-        const int dst = list[i], src = list[p.v.cap - 1 - i];
-        p.mass_out[base + dst] = mass[src];
-        p.pos_out[base + dst] = pos[src];
-    }
-    if (tid == 0) p.count[blockIdx.x] = freed;
+    if (tid == 0 && rank == 0) p.count[pair] = moved;
+    cluster_barrier();                                  // nobody leaves while its shared memory is read
 }
 
-constexpr int MV_WARPS = 8;
+constexpr int MV_WARPS = 8, MV_FLIGHT = 4;              // rows of a group of lanes in flight together
 
 template <int D>
 __global__ void __launch_bounds__(MV_WARPS * 32) evict_move_kernel(const EvictParams p) {
-    constexpr int LPR = D / 8;                          // lanes of a row of 16-byte units; K and V side by side fill a warp (d = 128)
+    constexpr int LPR = D / 8, LANES = 2 * LPR, PER = MV_WARPS * 32 / LANES;        // 16-byte units of a row; lanes of a row of K and one of V
     pdl_wait();
     pdl_release();
     if (*p.v.status != 0) return;
     const int pair = blockIdx.x / p.move_blocks, block = blockIdx.x % p.move_blocks, b = pair / p.v.Hkv, h = pair % p.v.Hkv;
     if (block == 0 && h == 0 && threadIdx.x == 0) p.lens_out[b] = min(p.v.lens[b], p.keep);
-    const int n = p.count[pair];
-    const int* list = p.list + (size_t)pair * p.v.cap;
-    const int unit = threadIdx.x % (2 * LPR), per = MV_WARPS * 32 / (2 * LPR);
-    __nv_bfloat16* T = unit < LPR ? p.K : p.V;
-    const int e0 = (unit % LPR) * 8;
-    for (int i = block * per + threadIdx.x / (2 * LPR); i < n; i += p.move_blocks * per) {
-        const long long to = load_pool_row(p.v, b, list[i]), from = load_pool_row(p.v, b, list[p.v.cap - 1 - i]);
-        if (to < 0 || from < 0) continue;
-        *reinterpret_cast<uint4*>(T + ((size_t)to * p.v.Hkv + h) * D + e0) = *reinterpret_cast<const uint4*>(T + ((size_t)from * p.v.Hkv + h) * D + e0);
+    const int n = p.count[pair], step = p.move_blocks * PER;
+    const size_t base = (size_t)pair * p.v.cap;
+    const int* list = p.list + base;
+    const int unit = threadIdx.x % LANES;
+    __nv_bfloat16* T = (unit < LPR ? p.K : p.V) + (size_t)h * D + (unit % LPR) * 8;
+    const size_t pitch = (size_t)p.v.Hkv * D;
+    for (int i0 = block * PER + threadIdx.x / LANES; i0 < n; i0 += MV_FLIGHT * step) {
+        int dst[MV_FLIGHT], src[MV_FLIGHT];
+        long long to[MV_FLIGHT], from[MV_FLIGHT];
+        uint4 x[MV_FLIGHT];
+#pragma unroll
+        for (int f = 0; f < MV_FLIGHT; ++f) {
+            const int i = i0 + f * step;
+            dst[f] = i < n ? list[i] : -1; src[f] = i < n ? list[p.v.cap - 1 - i] : -1;
+        }
+#pragma unroll
+        for (int f = 0; f < MV_FLIGHT; ++f) {
+            to[f] = from[f] = -1;
+            if (dst[f] >= 0) { to[f] = load_pool_row(p.v, b, dst[f]); from[f] = load_pool_row(p.v, b, src[f]); }
+        }
+#pragma unroll
+        for (int f = 0; f < MV_FLIGHT; ++f)
+            if (to[f] >= 0 && from[f] >= 0) x[f] = *reinterpret_cast<const uint4*>(T + (size_t)from[f] * pitch);
+#pragma unroll
+        for (int f = 0; f < MV_FLIGHT; ++f) {
+            if (to[f] >= 0 && from[f] >= 0) *reinterpret_cast<uint4*>(T + (size_t)to[f] * pitch) = x[f];
+            if (dst[f] >= 0 && unit == 0) { p.mass_out[base + dst[f]] = p.mass_in[base + src[f]]; p.pos_out[base + dst[f]] = p.pos_in[base + src[f]]; }
+        }
     }
 }
 
@@ -214,10 +325,18 @@ extern "C" seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_p
     p.list = reinterpret_cast<int*>(ws + w.evict_list_off);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const unsigned pairs = (unsigned)shape->batch * (unsigned)shape->n_kv_heads;
-    stc = launch_kernel(true, evict_select_kernel, dim3(pairs), EV_THREADS, 0, st, p);
-    if (stc != SEKA_OK) return stc;
     int n_sm = 0;
     if (!device_info(&n_sm)) return SEKA_ERR_CUDA;
+    // CTAs of a pair: more while they still find SMs and have 1024 rows each (a cache may be filled to its last page)
+    p.cluster = 1;
+    while (p.cluster < EV_MAX_CLUSTER && 2LL * p.cluster * pairs <= 2LL * n_sm && p.v.cap > 2 * 1024 * p.cluster) p.cluster *= 2;
+    const int lanes = p.cluster * EV_WARPS * 32;
+    const long long rows = ((long long)p.v.cap + lanes - 1) / lanes * (EV_WARPS * 32);      // most rows of a CTA
+    p.cached = rows <= EV_MAX_CACHED ? (int)rows : 0;                                       // longer: ranks are formed again in every pass
+    const size_t bytes = sizeof(EvSmem) + (size_t)p.cached * 5;
+    if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return SEKA_ERR_CUDA;
+    stc = launch_cluster(true, (unsigned)p.cluster, evict_select_kernel, dim3(pairs * (unsigned)p.cluster), EV_THREADS, bytes, st, p);
+    if (stc != SEKA_OK) return stc;
     const int D = shape->head_dim, per = MV_WARPS * 32 / (D / 4);
     const long long most = p.v.cap - keep < keep ? p.v.cap - keep : keep;          // rows of a pair that can move
     long long blocks = most > 0 ? (most + per - 1) / per : 1;

@@ -4,10 +4,11 @@
 // The angle in turns is reduced to [-1/2, 1/2] in fp64 (p turns_i is exact to 2^-53 of itself: 1e-9 of a turn at a position of
 // 10^7) and only then becomes fp32; products are fp32, each output is rounded once.
 //
-// Bound by HBM: every element is read once and written once.  A block takes one token (for few tokens several blocks share it, a
-// part of the heads each); its cosines and sines are computed once into shared memory.  A lane owns eight consecutive
-// elements of a head; a rotation in halves finds the partners of its elements, which lie r/2 away at no alignment, through a
-// copy of the row in shared memory that the lanes of one warp share.
+// Bound by HBM: every element is read once and written once.  A block takes a few tokens; their cosines and sines are computed once
+// into shared memory.  A lane owns 16 elements of a head, as eight pairs where it can:
+//   NEIGHBOURS  interleaved pairs: 16 consecutive elements, any r (also what is not rotated at all);
+//   HALVES      pairs r/2 apart with r a multiple of 16: eight elements and their eight partners, both on 16-byte boundaries;
+//   STAGED      pairs r/2 apart at no alignment: the warp's rows go through shared memory, a lane per pair there.
 #include "seka_kernels.h"
 #include "seka_paged.cuh"
 
@@ -28,118 +29,173 @@ struct RopeParams {
     float magnitude;
 };
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[16], int at) {
     if constexpr (sizeof(T) == 2) {
         const uint4 w = *reinterpret_cast<const uint4*>(p);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u[i]));
-            x[2 * i] = f.x; x[2 * i + 1] = f.y;
+            x[at + 2 * i] = f.x; x[at + 2 * i + 1] = f.y;
         }
     } else {
         const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        x[at] = a.x; x[at + 1] = a.y; x[at + 2] = a.z; x[at + 3] = a.w;
+        x[at + 4] = b.x; x[at + 5] = b.y; x[at + 6] = b.z; x[at + 7] = b.w;
     }
 }
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[16], int at) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[at], x[at + 1]), pack_bf16(x[at + 2], x[at + 3]), pack_bf16(x[at + 4], x[at + 5]), pack_bf16(x[at + 6], x[at + 7]));
+}
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void put(float& d, float x) { d = x; }
+__device__ __forceinline__ void put(__nv_bfloat16& d, float x) { d = __float2bfloat16(x); }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopeParams p) {
-    constexpr int LPR = D / 8, RPW = 32 / LPR;          // lanes of a row, rows of a warp
-    __shared__ float2 cs[D / 2];
-    __shared__ float rows[ROPE_THREADS / 32][RPW][D];
-    __shared__ int tok[4];                              // sequence, row in the cache (negative: padding), pool row
-    const int t = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+enum RopeMode { NEIGHBOURS, HALVES, STAGED };
+constexpr int ROPE_WARPS = ROPE_THREADS / 32, ROPE_TOKENS = 4;
+
+template <typename T, int D, RopeMode MODE>
+__global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopeParams p, int tokens) {
+    constexpr int LPR = D / 16, RPW = 32 / LPR;             // lanes of a row, rows of a warp
+    __shared__ __align__(16) float2 cs[ROPE_TOKENS][D / 2];
+    __shared__ int tok[ROPE_TOKENS][3];                     // sequence, row in the cache (negative: padding), pool row
+    __shared__ __align__(16) T stage[MODE == STAGED ? ROPE_WARPS : 1][MODE == STAGED ? RPW : 1][D];
+    const int t0 = (int)blockIdx.x * tokens, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int nt = min(tokens, p.v.T - t0);
     pdl_wait();
     pdl_release();
+    const int r = p.turns ? p.r : 0, half = r / 2;
     const int status0 = *p.v.status;
-    if (tid == 0) { tok[0] = -1; tok[1] = -1; tok[2] = -1; }
+    if (tid < ROPE_TOKENS) { tok[tid][0] = -1; tok[tid][1] = -1; tok[tid][2] = -1; }
     __syncthreads();
     if (status0 != 0) return;
-    // the sequence that owns the token
+    // the sequences that own the tokens
     for (int b = tid; b < p.v.B; b += ROPE_THREADS) {
         const int q0 = p.v.cu ? p.v.cu[b] : b * p.v.max_new, q1 = p.v.cu ? p.v.cu[b + 1] : q0 + p.v.max_new;
-        if (t < q0 || t >= q1) continue;
+        if (q0 >= t0 + nt || q1 <= t0) continue;
         const PagedSeq s = check_seq(p.v, q0, q1, p.v.lens[b]);
         if (!s.valid) { report_invalid(p.v.status, kWhereSeq); continue; }
-        const int j = s.L - s.n + (t - q0);
-        tok[0] = b; tok[1] = j;
-        if (j >= 0) tok[2] = (int)load_pool_row(p.v, b, j);
-    }
-    __syncthreads();
-    const int b = tok[0], j = tok[1];
-    const long long row = tok[2];
-    if (p.turns != nullptr && tid < p.r / 2) {
-        const int pos = p.positions ? p.positions[t] : j;
-        double a = (double)pos * p.turns[tid];
-        a -= rint(a);
-        float s, c;
-        sincospif(2.f * (float)a, &s, &c);
-        cs[tid] = make_float2(c * p.magnitude, s * p.magnitude);
-    }
-    __syncthreads();
-    const int Hq = p.v.Hq, Hkv = p.v.Hkv, n_rows = Hq + 2 * Hkv, r = p.turns ? p.r : 0, half = r / 2;
-    const int sub = lane / LPR, e0 = (lane % LPR) * 8;
-    const int first = ((int)blockIdx.y * (ROPE_THREADS / 32) + warp) * RPW;
-    for (int h0 = first; h0 < n_rows; h0 += (int)gridDim.y * (ROPE_THREADS / 32) * RPW) {
-        const int h = h0 + sub;
-        const bool isq = h < Hq, isk = !isq && h < Hq + Hkv, have = h < n_rows && (isq || row >= 0);
-        const bool turn = have && (isq || isk) && e0 < r;
-        float x[8];
-        if (have) {
-            const T* src = isq ? static_cast<const T*>(p.Q) + t * p.q_stride + (size_t)h * D
-                         : isk ? static_cast<const T*>(p.K) + t * p.k_stride + (size_t)(h - Hq) * D
-                               : static_cast<const T*>(p.V) + t * p.v_stride + (size_t)(h - Hq - Hkv) * D;
-            load8(src + e0, x);
+        for (int i = max(0, q0 - t0); i < min(nt, q1 - t0); ++i) {
+            const int j = s.L - s.n + (t0 + i - q0);
+            tok[i][0] = b; tok[i][1] = j;
+            if (j >= 0) tok[i][2] = (int)load_pool_row(p.v, b, j);
         }
-        if (p.layout == SEKA_ROPE_INTERLEAVED) {
-            if (turn) {
+    }
+    if (p.positions == nullptr) __syncthreads();
+    for (int x = tid; x < nt * half; x += ROPE_THREADS) {
+        const int i = x / half, k = x - i * half;
+        const int pos = p.positions ? p.positions[t0 + i] : tok[i][1];
+        double a = (double)pos * p.turns[k];
+        a -= rint(a);
+        float sn, c;
+        sincospif(2.f * (float)a, &sn, &c);
+        cs[i][k] = make_float2(c * p.magnitude, sn * p.magnitude);
+    }
+    __syncthreads();
+    const int Hq = p.v.Hq, Hkv = p.v.Hkv, n_rows = Hq + 2 * Hkv, groups = (n_rows + RPW - 1) / RPW;
+    const int sub = lane / LPR, q = lane % LPR;
+    // the lane's two runs of eight elements: pair i is (x[i], x[8 + i]) (HALVES) or (x[2 i], x[2 i + 1]) of them
+    const bool apart = MODE == HALVES && 16 * q < r;
+    const int e0 = apart ? 8 * q : 16 * q, e1 = apart ? half + 8 * q : 16 * q + 8;
+    struct Row { int i, h; long long row; bool have, turn; };
+    auto row_of = [&](int k) -> Row {
+        Row w;
+        w.i = k / groups;
+        w.h = (k - w.i * groups) * RPW + sub;
+        w.row = w.i < nt ? (long long)tok[w.i][2] : -1;
+        w.have = w.i < nt && w.h < n_rows && (w.h < Hq || w.row >= 0);
+        w.turn = w.have && w.h < Hq + Hkv;
+        return w;
+    };
+    auto load = [&](const Row& w, float (&x)[16]) {
+        if (!w.have) return;
+        const size_t t = (size_t)(t0 + w.i);
+        const T* src = w.h < Hq ? static_cast<const T*>(p.Q) + t * p.q_stride + (size_t)w.h * D
+                     : w.h < Hq + Hkv ? static_cast<const T*>(p.K) + t * p.k_stride + (size_t)(w.h - Hq) * D
+                                      : static_cast<const T*>(p.V) + t * p.v_stride + (size_t)(w.h - Hq - Hkv) * D;
+        load8(src + e0, x, 0);
+        load8(src + e1, x, 8);
+    };
+    auto finish = [&](const Row& w, float (&x)[16]) {
+        if (MODE == STAGED) {
+            T* mine = stage[warp][sub];
+            __syncwarp();                                   // the rows before have been read
+            if (w.turn) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (e0 + 2 * i < r) {
-                        const float2 c = cs[e0 / 2 + i];
-                        const float u = x[2 * i], w = x[2 * i + 1];
-                        x[2 * i] = u * c.x - w * c.y; x[2 * i + 1] = w * c.x + u * c.y;
+                for (int i = 0; i < 16; i += 8) {
+                    if constexpr (sizeof(T) == 2) store8(mine + e0 + i, x, i);
+                    else {
+                        *reinterpret_cast<float4*>(mine + e0 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                        *reinterpret_cast<float4*>(mine + e0 + i + 4) = make_float4(x[i + 4], x[i + 5], x[i + 6], x[i + 7]);
                     }
-            }
-        } else {
-            float* mine = rows[warp][sub];
-            __syncwarp();                               // the partners of the row before have been read
-            if (turn) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) mine[e0 + i] = x[i];
+                }
             }
             __syncwarp();
-            if (turn) {
+            const int i = min(w.i, nt - 1);                 // (the rows of a warp belong to one token)
+            for (int k = lane; k < half; k += 32) {
+                const float2 c = cs[i][k];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int e = e0 + i;
-                    if (e < half) { const float2 c = cs[e]; x[i] = x[i] * c.x - mine[e + half] * c.y; }
-                    else if (e < r) { const float2 c = cs[e - half]; x[i] = x[i] * c.x + mine[e - half] * c.y; }
+                for (int y = 0; y < RPW; ++y) {             // rows that are not turned hold what nobody reads
+                    const float a = to_f32(stage[warp][y][k]), b = to_f32(stage[warp][y][k + half]);
+                    put(stage[warp][y][k], a * c.x - b * c.y);
+                    put(stage[warp][y][k + half], b * c.x + a * c.y);
+                }
+            }
+            __syncwarp();
+            if (w.turn) { load8(mine + e0, x, 0); load8(mine + e1, x, 8); }
+        } else if (w.turn && 16 * q < r) {
+            const float4* c4 = reinterpret_cast<const float4*>(&cs[w.i][8 * q]);
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float4 c = c4[k / 2];                 // of pairs 8 q + k and the next; behind r/2: not used
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float cx = y ? c.z : c.x, sx = y ? c.w : c.y;
+                    float& a = MODE == HALVES ? x[k + y] : x[2 * (k + y)];
+                    float& b = MODE == HALVES ? x[8 + k + y] : x[2 * (k + y) + 1];
+                    const float ya = a * cx - b * sx, yb = b * cx + a * sx;
+                    if (MODE == HALVES || 8 * q + k + y < half) { a = ya; b = yb; }
                 }
             }
         }
-        if (have) {
-            __nv_bfloat16* dst = isq ? p.Q_out + ((size_t)t * Hq + h) * D
-                               : isk ? p.K_pages + ((size_t)row * Hkv + (h - Hq)) * D : p.V_pages + ((size_t)row * Hkv + (h - Hq - Hkv)) * D;
-            *reinterpret_cast<uint4*>(dst + e0) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-        }
+        if (!w.have) return;
+        __nv_bfloat16* dst = w.h < Hq ? p.Q_out + ((size_t)(t0 + w.i) * Hq + w.h) * D
+                           : w.h < Hq + Hkv ? p.K_pages + ((size_t)w.row * Hkv + (w.h - Hq)) * D
+                                            : p.V_pages + ((size_t)w.row * Hkv + (w.h - Hq - Hkv)) * D;
+        store8(dst + e0, x, 0);
+        store8(dst + e1, x, 8);
+    };
+    const int step = ROPE_WARPS * (int)gridDim.y;
+    for (int k = (int)blockIdx.y * ROPE_WARPS + warp; k < nt * groups; k += 2 * step) {     // two groups' loads in flight
+        const Row wa = row_of(k), wb = row_of(k + step);
+        float xa[16], xb[16];
+        load(wa, xa);
+        load(wb, xb);
+        finish(wa, xa);
+        finish(wb, xb);
     }
-    if (p.pos_cache != nullptr && blockIdx.y == 0 && row >= 0)
-        for (int h = tid; h < Hkv; h += ROPE_THREADS)
-            p.pos_cache[((size_t)b * Hkv + h) * p.v.cap + j] = p.positions ? p.positions[t] : j;
+    if (p.pos_cache != nullptr && blockIdx.y == 0)
+        for (int x = tid; x < nt * Hkv; x += ROPE_THREADS) {
+            const int i = x % nt, h = x / nt;               // neighbouring tokens are neighbours in the cache
+            if (tok[i][2] >= 0)
+                p.pos_cache[((size_t)tok[i][0] * Hkv + h) * p.v.cap + tok[i][1]] = p.positions ? p.positions[t0 + i] : tok[i][1];
+        }
 }
 
-template <typename T>
-seka_status launch_rope(const RopeParams& p, int D, cudaStream_t st) {
+template <typename T, int D>
+seka_status launch_rope(const RopeParams& p, cudaStream_t st) {
     int n_sm = 0;
     if (!device_info(&n_sm)) return SEKA_ERR_CUDA;
-    const int per = ROPE_THREADS / 32 * (32 * 8 / D), n_rows = p.v.Hq + 2 * p.v.Hkv;
-    int split = 1;                  // blocks of a token: as many as fill the SMs, no more than it has rows for
-    while (split * per < n_rows && (long long)p.v.T * split < 2LL * n_sm) ++split;
-    const dim3 grid((unsigned)p.v.T, (unsigned)split);
-    return D == 128 ? launch_kernel(true, rope_append_kernel<T, 128>, grid, ROPE_THREADS, 0, st, p)
-                    : launch_kernel(true, rope_append_kernel<T, 64>, grid, ROPE_THREADS, 0, st, p);
+    const int groups = (p.v.Hq + 2 * p.v.Hkv + 512 / D - 1) / (512 / D);        // of a token's rows: a warp's worth each
+    // four tokens a block where that still gives every SM a few blocks; else one, and blocks share a token as far as it has rows
+    const int tokens = p.v.T >= ROPE_TOKENS * 4 * n_sm ? ROPE_TOKENS : 1;
+    int split = 1;
+    while (tokens == 1 && split * ROPE_WARPS < groups && (long long)p.v.T * split < 2LL * n_sm) ++split;
+    const dim3 grid((unsigned)((p.v.T + tokens - 1) / tokens), (unsigned)split);
+    const bool halves = p.turns != nullptr && p.layout == SEKA_ROPE_HALF;
+    auto kern = !halves ? rope_append_kernel<T, D, NEIGHBOURS> : p.r % 16 == 0 ? rope_append_kernel<T, D, HALVES> : rope_append_kernel<T, D, STAGED>;
+    return launch_kernel(true, kern, grid, ROPE_THREADS, 0, st, p, tokens);
 }
 
 }  // namespace
@@ -179,5 +235,6 @@ extern "C" seka_status seka_rope_append(const seka_paged_shape* shape, const sek
     p.turns = rope ? rope->turns : nullptr; p.r = rope ? rope->rot_dim : 0; p.layout = rope ? rope->layout : 0;
     p.magnitude = rope && rope->magnitude > 0.f ? rope->magnitude : 1.f;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return shape->dtype == SEKA_F32 ? launch_rope<float>(p, D, st) : launch_rope<__nv_bfloat16>(p, D, st);
+    return shape->dtype == SEKA_F32 ? (D == 128 ? launch_rope<float, 128>(p, st) : launch_rope<float, 64>(p, st))
+                                    : (D == 128 ? launch_rope<__nv_bfloat16, 128>(p, st) : launch_rope<__nv_bfloat16, 64>(p, st));
 }

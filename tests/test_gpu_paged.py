@@ -270,6 +270,15 @@ def test_evict(lens, Hkv, d, page, keep, recent, share, kind):
     run_evict(c, m.cuda(), pos.cuda(), None if protect is None else protect.cuda(), next_pos.cuda(), keep, recent)
 
 
+def test_evict_long_rows_and_many_pairs():
+    # one sequence whose ranks do not fit in a CTA's shared memory, in a batch that leaves each pair one CTA
+    c = R.Cache([40000] + [20] * 37, [0] * 38, 4, 4, 64, 256, seed=12)
+    m = torch.randn((c.B, 4, c.cap), generator=c.g).mul(1.5).exp().cuda()
+    pos = torch.arange(c.cap, dtype=torch.int32).expand(c.B, 4, -1).contiguous().cuda()
+    protect = (torch.rand((c.B, 30000), generator=c.g) < 0.2).to(torch.uint8).cuda()
+    run_evict(c, m, pos, protect, c.lens_d.clone(), 15000, 100)
+
+
 def test_evict_in_place_and_again():
     c = R.Cache([900, 64], [0, 0], 2, 2, 64, 16, seed=9)
     m = torch.rand((2, 2, c.cap), generator=c.g).cuda()
