@@ -971,7 +971,7 @@ static EncodeTiledFn encode_tiled_fn() {
 }
 
 // bf16 tensor [T, H, d] viewed as (d, H, T); tiles of 64 x box_heads x box_rows with the 128-byte swizzle.
-bool make_tile_map(CUtensorMap* m, const void* base, int d, int H, long long T, int box_rows, int box_heads) {
+bool make_tile_map(CUtensorMap* m, const void* base, int d, int H, long long T, int box_rows, int box_heads, bool narrow) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (fn == nullptr) return false;
     cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)H, (cuuint64_t)T};
@@ -979,7 +979,7 @@ bool make_tile_map(CUtensorMap* m, const void* base, int d, int H, long long T, 
     cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
     cuuint32_t estr[3] = {1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, narrow ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

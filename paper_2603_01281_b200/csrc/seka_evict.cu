@@ -4,7 +4,7 @@
 //                         recent, 1: highlighted, 0) above its weight mapped to 32 bits whose unsigned order is the order of the
 //                         weights; both are formed once and kept in shared memory (where they fit).  The class that the keep-th row
 //                         belongs to follows from the counts, its weight is found in four digits of eight bits: a CTA's
-//                         histogram has a column per lane (256 x 32 words: a warp's updates never meet), the CTAs add their totals through
+//                         histogram has 16 columns (a warp's updates meet in pairs at most), the CTAs add their totals through
 //                         distributed shared memory.  Then ties by row, and the lists of the freed rows below `keep` and the
 //                         kept ones behind, every warp on consecutive rows so that ranks come from ballots.
 //   evict_move_kernel     copies K, V, weight and position of the kept rows behind into the freed rows.
@@ -20,7 +20,9 @@ namespace {
 
 constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
 constexpr int EV_MAX_CLUSTER = 8;
-constexpr int EV_MAX_CACHED = 36 * 1024;                // rows of a CTA whose ranks fit in shared memory beside the histogram
+constexpr int EV_COLS = 16;                             // columns of the histogram (lanes l and l + 16 share one); 32 leave too little room for four CTAs per SM
+constexpr int EV_FLIGHT = 8;                            // rows of a lane whose loads are in flight together
+constexpr int EV_MAX_CACHED = 40 * 1024;                // rows of a CTA whose ranks fit in shared memory beside the histogram
 
 struct EvictParams {
     PagedView v;
@@ -48,7 +50,7 @@ SEKA_HD uint32_t mass_order(float x, uint32_t bits) {
 }
 
 struct EvSmem {
-    int hist[256][32];
+    int hist[256][EV_COLS];
     int tot[2][256];            // this CTA's totals of a digit (read by the cluster; two, so that one barrier per digit is enough)
     int sum[256];
     int xch[3][4];              // what the CTAs tell each other: class counts and status; ties; freed and late rows
@@ -102,25 +104,47 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
     const int wlo = hi - lo < warp * wrows ? hi : lo + warp * wrows, whi = hi - wlo < wrows ? hi : wlo + wrows;
     const bool cached = chunk <= p.cached;
     const long long recent_from = (long long)p.next_pos[b] - p.recent;
-    auto rank_of = [&](int j, uint32_t& o) -> int {     // class, and the weight's order
+    auto class_of = [&](int x, int flag) -> int { return (long long)x >= recent_from ? 2 : flag; };
+    // where the flag of a position lies (any valid address where it has none), and whether it has one
+    const uint8_t* prot = p.protect != nullptr ? p.protect + (size_t)b * p.protect_len : nullptr;
+    auto flag_of = [&](int x) -> int {
+        const bool inside = x >= 0 && x < p.protect_len;
+        const int f = prot != nullptr ? (int)prot[inside ? x : 0] : 0;
+        return inside && f != 0 ? 1 : 0;
+    };
+    auto get = [&](int j, uint32_t& o) -> int {         // class, and the weight's order
+        if (cached) { o = ord_s[j - lo]; return cls_s[j - lo]; }
         const float m = mass[j];
         const int x = pos[j];
         o = mass_order(m, __float_as_uint(m));
-        if ((long long)x >= recent_from) return 2;
-        return (p.protect != nullptr && x >= 0 && x < p.protect_len && p.protect[(size_t)b * p.protect_len + x] != 0) ? 1 : 0;
+        return class_of(x, flag_of(x));
     };
-    auto get = [&](int j, uint32_t& o) -> int {
-        if (!cached) return rank_of(j, o);
-        o = ord_s[j - lo];
-        return cls_s[j - lo];
-    };
+    // weights and positions once from memory, several rows' loads in flight; rows below `keep` are passed on as they are (what is freed
+    // is written over by the second launch)
     int n2 = 0, n1 = 0;
-#pragma unroll 4
-    for (int j = wlo + lane; j < whi; j += 32) {
-        uint32_t o;
-        const int c = rank_of(j, o);
-        if (cached) { ord_s[j - lo] = o; cls_s[j - lo] = (uint8_t)c; }
-        n2 += c == 2; n1 += c == 1;
+    const bool copy_m = p.mass_out != p.mass_in, copy_p = p.pos_out != p.pos_in;
+    for (int j0 = wlo + lane; j0 - lane < whi; j0 += 32 * EV_FLIGHT) {
+        float m[EV_FLIGHT];
+        int x[EV_FLIGHT], f[EV_FLIGHT];
+#pragma unroll
+        for (int i = 0; i < EV_FLIGHT; ++i) {
+            const int j = min(j0 + 32 * i, whi - 1);    // (the last row again where there is none)
+            m[i] = mass[j]; x[i] = pos[j];
+        }
+#pragma unroll
+        for (int i = 0; i < EV_FLIGHT; ++i) f[i] = flag_of(x[i]);
+#pragma unroll
+        for (int i = 0; i < EV_FLIGHT; ++i) {
+            const int j = j0 + 32 * i;
+            if (j >= whi) continue;
+            const int c = class_of(x[i], f[i]);
+            if (cached) { ord_s[j - lo] = mass_order(m[i], __float_as_uint(m[i])); cls_s[j - lo] = (uint8_t)c; }
+            n2 += c == 2; n1 += c == 1;
+            if (j < keep) {
+                if (copy_m) p.mass_out[base + j] = m[i];
+                if (copy_p) p.pos_out[base + j] = x[i];
+            }
+        }
     }
     n2 = __reduce_add_sync(all, n2); n1 = __reduce_add_sync(all, n1);
     if (lane == 0) { sm.warp_a[warp] = n2; sm.warp_b[warp] = n1; }
@@ -142,18 +166,20 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
     for (int digit = 0; digit < 4; ++digit) {
         const int shift = 24 - 8 * digit;
         const uint32_t above = digit == 0 ? 0u : 0xffffffffu << (shift + 8);
-        for (int i = tid; i < 256 * 32 / 4; i += EV_THREADS) reinterpret_cast<int4*>(&sm.hist[0][0])[i] = make_int4(0, 0, 0, 0);
+        for (int i = tid; i < 256 * EV_COLS / 4; i += EV_THREADS) reinterpret_cast<int4*>(&sm.hist[0][0])[i] = make_int4(0, 0, 0, 0);
         __syncthreads();
 #pragma unroll 4
         for (int j = wlo + lane; j < whi; j += 32) {
             uint32_t o;
             const int c = get(j, o);
-            if (c == cut_class && (o & above) == cut) atomicAdd(&sm.hist[(o >> shift) & 255][lane], 1);
+            if (c == cut_class && (o & above) == cut) atomicAdd(&sm.hist[(o >> shift) & 255][lane % EV_COLS], 1);
         }
         __syncthreads();
-        for (int i = warp; i < 256; i += EV_WARPS) {
-            const int x = __reduce_add_sync(all, sm.hist[i][lane]);
-            if (lane == 0) sm.tot[digit & 1][i] = x;
+        if (tid < 256) {                                // (rotated: neighbouring bins start in other banks)
+            int x = 0;
+#pragma unroll
+            for (int i = 0; i < EV_COLS; ++i) x += sm.hist[tid][(i + (tid >> 1)) % EV_COLS];
+            sm.tot[digit & 1][tid] = x;
         }
         cluster_barrier();
         if (tid < 256) {
@@ -246,52 +272,53 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
         if (gone) list[at_f + __popc(bf & below)] = j;
         if (back) list[p.v.cap - 1 - (at_l + __popc(bl & below))] = j;
         at_f += __popc(bf); at_l += __popc(bl);
-        if (j < keep && in) {
-            if (p.mass_out != p.mass_in) p.mass_out[base + j] = mass[j];
-            if (p.pos_out != p.pos_in) p.pos_out[base + j] = pos[j];
-        }
     }
     if (tid == 0 && rank == 0) p.count[pair] = moved;
     cluster_barrier();                                  // nobody leaves while its shared memory is read
 }
 
-constexpr int MV_WARPS = 8, MV_FLIGHT = 4;              // rows of a group of lanes in flight together
+// A warp takes 32 rows of the list: its lanes look up places and pages of a row each, then the rows are copied eight at a time.
+constexpr int MV_WARPS = 8;
 
 template <int D>
 __global__ void __launch_bounds__(MV_WARPS * 32) evict_move_kernel(const EvictParams p) {
-    constexpr int LPR = D / 8, LANES = 2 * LPR, PER = MV_WARPS * 32 / LANES;        // 16-byte units of a row; lanes of a row of K and one of V
+    constexpr int LPR = D / 8, LANES = 2 * LPR, TOGETHER = 32 / LANES, FLIGHT = 8;      // 16-byte units of a row; lanes of a row of K and one of V
     pdl_wait();
     pdl_release();
-    if (*p.v.status != 0) return;
+    const int status0 = *p.v.status;
     const int pair = blockIdx.x / p.move_blocks, block = blockIdx.x % p.move_blocks, b = pair / p.v.Hkv, h = pair % p.v.Hkv;
+    const int n = p.count[pair], lane = threadIdx.x & 31;
+    if (status0 != 0) return;
     if (block == 0 && h == 0 && threadIdx.x == 0) p.lens_out[b] = min(p.v.lens[b], p.keep);
-    const int n = p.count[pair], step = p.move_blocks * PER;
     const size_t base = (size_t)pair * p.v.cap;
-    const int* list = p.list + base;
-    const int unit = threadIdx.x % LANES;
+    const int unit = lane % LANES, which = lane / LANES;
     __nv_bfloat16* T = (unit < LPR ? p.K : p.V) + (size_t)h * D + (unit % LPR) * 8;
     const size_t pitch = (size_t)p.v.Hkv * D;
-    for (int i0 = block * PER + threadIdx.x / LANES; i0 < n; i0 += MV_FLIGHT * step) {
-        int dst[MV_FLIGHT], src[MV_FLIGHT];
-        long long to[MV_FLIGHT], from[MV_FLIGHT];
-        uint4 x[MV_FLIGHT];
-#pragma unroll
-        for (int f = 0; f < MV_FLIGHT; ++f) {
-            const int i = i0 + f * step;
-            dst[f] = i < n ? list[i] : -1; src[f] = i < n ? list[p.v.cap - 1 - i] : -1;
+    for (int i0 = (block * MV_WARPS + (threadIdx.x >> 5)) * 32; i0 < n; i0 += p.move_blocks * MV_WARPS * 32) {
+        const int i = i0 + lane, rows = min(32, n - i0);
+        int to = -1, from = -1;
+        if (i < n) {
+            const int dst = p.list[base + i], src = p.list[base + p.v.cap - 1 - i];
+            const float m = p.mass_in[base + src];
+            const int x = p.pos_in[base + src];
+            to = (int)load_pool_row(p.v, b, dst); from = (int)load_pool_row(p.v, b, src);
+            if (from < 0) to = -1;
+            p.mass_out[base + dst] = m;
+            p.pos_out[base + dst] = x;
         }
+        for (int k0 = 0; k0 < rows; k0 += FLIGHT * TOGETHER) {
+            uint4 x[FLIGHT];
+            int t[FLIGHT];
 #pragma unroll
-        for (int f = 0; f < MV_FLIGHT; ++f) {
-            to[f] = from[f] = -1;
-            if (dst[f] >= 0) { to[f] = load_pool_row(p.v, b, dst[f]); from[f] = load_pool_row(p.v, b, src[f]); }
-        }
+            for (int f = 0; f < FLIGHT; ++f) {
+                const int k = k0 + f * TOGETHER + which;                    // (below 32; rows that do not exist have no place)
+                t[f] = __shfl_sync(0xffffffffu, to, k & 31);
+                const int s = __shfl_sync(0xffffffffu, from, k & 31);
+                if (t[f] >= 0) x[f] = *reinterpret_cast<const uint4*>(T + (size_t)s * pitch);
+            }
 #pragma unroll
-        for (int f = 0; f < MV_FLIGHT; ++f)
-            if (to[f] >= 0 && from[f] >= 0) x[f] = *reinterpret_cast<const uint4*>(T + (size_t)from[f] * pitch);
-#pragma unroll
-        for (int f = 0; f < MV_FLIGHT; ++f) {
-            if (to[f] >= 0 && from[f] >= 0) *reinterpret_cast<uint4*>(T + (size_t)to[f] * pitch) = x[f];
-            if (dst[f] >= 0 && unit == 0) { p.mass_out[base + dst[f]] = p.mass_in[base + src[f]]; p.pos_out[base + dst[f]] = p.pos_in[base + src[f]]; }
+            for (int f = 0; f < FLIGHT; ++f)
+                if (t[f] >= 0) *reinterpret_cast<uint4*>(T + (size_t)t[f] * pitch) = x[f];
         }
     }
 }
@@ -337,10 +364,10 @@ extern "C" seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_p
     if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return SEKA_ERR_CUDA;
     stc = launch_cluster(true, (unsigned)p.cluster, evict_select_kernel, dim3(pairs * (unsigned)p.cluster), EV_THREADS, bytes, st, p);
     if (stc != SEKA_OK) return stc;
-    const int D = shape->head_dim, per = MV_WARPS * 32 / (D / 4);
+    const int D = shape->head_dim;
     const long long most = p.v.cap - keep < keep ? p.v.cap - keep : keep;          // rows of a pair that can move
-    long long blocks = most > 0 ? (most + per - 1) / per : 1;
-    const long long fill = (8LL * n_sm + pairs - 1) / pairs;
+    long long blocks = most > 0 ? (most + MV_WARPS * 32 - 1) / (MV_WARPS * 32) : 1;
+    const long long fill = (16LL * n_sm + pairs - 1) / pairs;
     if (blocks > fill) blocks = fill;
     p.move_blocks = (int)blocks;
     const dim3 grid(pairs * (unsigned)blocks);

@@ -40,7 +40,8 @@ seka_status launch_route(const seka_shape* s, const void* Q, const float* U, con
                          float* alpha_out, cudaStream_t st);
 
 // bf16 tensor [T, H, d] viewed as (d, H, T) for TMA: tiles of 64 x box_heads x box_rows with the 128-byte swizzle.
-bool make_tile_map(CUtensorMap* m, const void* base, int d, int H, long long T, int box_rows = 128, int box_heads = 1);
+bool make_tile_map(CUtensorMap* m, const void* base, int d, int H, long long T, int box_rows = 128, int box_heads = 1,
+                   bool narrow = false);     // narrow: misses fetch 128 bytes into L2 instead of 256 (rows of 128 bytes, read a head at a time)
 
 // bf16 tensor [T, cols] for gathers of four rows x 64 columns at a time, 128-byte swizzle.
 bool make_row_map(CUtensorMap* m, const void* base, int cols, long long T);

@@ -530,14 +530,14 @@ extern "C" seka_status seka_attention_mass(const seka_paged_shape* shape, const 
         const int ctas = D == 128 ? MfSmem<128>::CTAS_PER_SM : MfSmem<64>::CTAS_PER_SM;
         const long long most = (pairs * ((p.v.cap + 63) / 64) + p.key.min_share - 1) / p.key.min_share;
         p.n_shares = (int)(most < kShareSms * ctas ? most : kShareSms * ctas);
-        if (!make_tile_map(&tk, K_pages, D, Hkv, pool, shape->page_size < MF_KEYS ? shape->page_size : MF_KEYS)) return SEKA_ERR_CUDA;
+        if (!make_tile_map(&tk, K_pages, D, Hkv, pool, shape->page_size < MF_KEYS ? shape->page_size : MF_KEYS, 1, D == 64)) return SEKA_ERR_CUDA;
         const bool half = shape->max_new * G <= 8;
         return D == 128 ? (half ? launch_mass_few<128, true>(tk, p, st) : launch_mass_few<128, false>(tk, p, st))
                         : (half ? launch_mass_few<64, true>(tk, p, st) : launch_mass_few<64, false>(tk, p, st));
     }
     const long long most = pairs * ((p.v.cap + 255) / 256) * p.rowg.tiles(shape->max_new);
     p.n_shares = (int)(most < kShareSms * p.rowg.min_share ? (most + p.rowg.min_share - 1) / p.rowg.min_share : kShareSms);
-    if (!make_tile_map(&tk, K_pages, D, Hkv, pool, shape->page_size < 128 ? shape->page_size : 128) ||
+    if (!make_tile_map(&tk, K_pages, D, Hkv, pool, shape->page_size < 128 ? shape->page_size : 128, 1, D == 64) ||
         !make_tile_map(&tq, Q, D, shape->n_q_heads, shape->total_new, p.rowg.tp, G)) return SEKA_ERR_CUDA;
     return D == 128 ? launch_mass_tiles<128>(tq, tk, p, st) : launch_mass_tiles<64>(tq, tk, p, st);
 }

@@ -295,57 +295,88 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
     }
 }
 
-// A block per (cut, eight rows): nothing to do where the share begins with a unit, or where an earlier cut of the same unit does it.
-constexpr int MERGE_WARPS = 8;
+// A block per (cut, 32 rows; 16 where a unit has no more): nothing to do where the share begins with a unit, or where an earlier cut of
+// the same unit does it.  A warp merges four rows at a time: the chain from the cut's record to the parts is four trips to memory long.
+constexpr int MERGE_WARPS = 8, MERGE_ROWS = 4;
 template <int D>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttnParams p, int unit_rows) {
     constexpr int E = D / 32;
-    const int blocks = unit_rows / MERGE_WARPS, cut = (int)blockIdx.x / blocks;
-    const int r = ((int)blockIdx.x - cut * blocks) * MERGE_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int blocks = (unit_rows + MERGE_WARPS * MERGE_ROWS - 1) / (MERGE_WARPS * MERGE_ROWS), cut = (int)blockIdx.x / blocks;
+    const int r0 = (((int)blockIdx.x - cut * blocks) * MERGE_WARPS + (threadIdx.x >> 5)) * MERGE_ROWS, lane = threadIdx.x & 31;
     pdl_wait();
     pdl_release();
-    if (*p.v.status != 0) return;
+    const int status0 = *p.v.status;
     const CutRecord c = p.cuts[cut];
-    if (c.n == 0 || c.j == 0 || c.j > c.share) return;
-    // row -> new token and query head
-    const int tile = r >> 7, rt = r & 127, t_tile = rt / p.v.G, tok = c.p * p.geo.tp + tile * p.tile_tokens + t_tile;
+    if (status0 != 0 || r0 >= unit_rows || c.n == 0 || c.j == 0 || c.j > c.share) return;
     const PagedSeq s = paged_seq(p.v, c.b);
-    if (t_tile >= p.tile_tokens || tok >= s.n) return;
-    const size_t out = (size_t)(s.q0 + tok) * p.v.Hq + (size_t)c.h * p.v.G + (rt - t_tile * p.v.G);
     // parts: the last segment of share cut - 1, then the first ones of the shares on
     const int parts = 1 + (c.n - c.j + c.share - 1) / c.share;
     auto slot = [&](int i) -> size_t { return i == 0 ? (size_t)(cut - 1) * 2 + (c.j < c.share ? 1 : 0) : (size_t)(cut - 1 + i) * 2; };
-    float M = -INFINITY, l = 0.f, acc[E] = {};
+    size_t out[MERGE_ROWS];
+    bool real[MERGE_ROWS];
+    bool any = false;
+#pragma unroll
+    for (int q = 0; q < MERGE_ROWS; ++q) {                  // row -> new token and query head
+        const int r = r0 + q, tile = r >> 7, rt = r & 127, t_tile = rt / p.v.G, tok = c.p * p.geo.tp + tile * p.tile_tokens + t_tile;
+        real[q] = t_tile < p.tile_tokens && tok < s.n;
+        out[q] = (size_t)(s.q0 + tok) * p.v.Hq + (size_t)c.h * p.v.G + (rt - t_tile * p.v.G);
+        any |= real[q];
+    }
+    if (!any) return;
+    float M[MERGE_ROWS], l[MERGE_ROWS], acc[MERGE_ROWS][E];
+#pragma unroll
+    for (int q = 0; q < MERGE_ROWS; ++q) {
+        M[q] = -INFINITY; l[q] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[q][e] = 0.f;
+    }
     for (int i0 = 0; i0 < parts; i0 += 32) {
         const int n = min(32, parts - i0);
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (lane < n) ml = *reinterpret_cast<const float2*>(p.part_ml + (slot(i0 + lane) * unit_rows + r) * 2);
-        float mx = fmaxf(M, ml.x);
+        float2 ml[MERGE_ROWS];
+        float f[MERGE_ROWS];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float keep = M == -INFINITY ? 0.f : fast_exp2(M - mx), f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - mx);
-        l = fmaf(l, keep, ml.y * f);                        // per lane until the end
-        M = mx;
+        for (int q = 0; q < MERGE_ROWS; ++q)
+            ml[q] = lane < n ? *reinterpret_cast<const float2*>(p.part_ml + (slot(i0 + lane) * unit_rows + r0 + q) * 2) : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= keep;
-#pragma unroll 8
+        for (int q = 0; q < MERGE_ROWS; ++q) {
+            float mx = fmaxf(M[q], ml[q].x);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const float keep = M[q] == -INFINITY ? 0.f : fast_exp2(M[q] - mx);
+            f[q] = ml[q].x == -INFINITY ? 0.f : fast_exp2(ml[q].x - mx);
+            l[q] = fmaf(l[q], keep, ml[q].y * f[q]);        // per lane until the end
+            M[q] = mx;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[q][e] *= keep;
+        }
+#pragma unroll 2
         for (int i = 0; i < n; ++i) {
-            const float fi = __shfl_sync(0xffffffffu, f, i);
-            const float* src = p.part_o + (slot(i0 + i) * unit_rows + r) * D + lane * E;
-            float x[E];
-            if (E == 4) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(src);
-            else *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(src);
+            const float* src = p.part_o + (slot(i0 + i) * unit_rows + r0) * D + lane * E;
+            float x[MERGE_ROWS][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(x[e], fi, acc[e]);
+            for (int q = 0; q < MERGE_ROWS; ++q) {
+                if (E == 4) *reinterpret_cast<float4*>(x[q]) = *reinterpret_cast<const float4*>(src + q * D);
+                else *reinterpret_cast<float2*>(x[q]) = *reinterpret_cast<const float2*>(src + q * D);
+            }
+#pragma unroll
+            for (int q = 0; q < MERGE_ROWS; ++q) {
+                const float fi = __shfl_sync(0xffffffffu, f[q], i);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[q][e] = fmaf(x[q][e], fi, acc[q][e]);
+            }
         }
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint32_t* dst = reinterpret_cast<uint32_t*>(p.O + out * D + lane * E);
+    for (int q = 0; q < MERGE_ROWS; ++q) {
 #pragma unroll
-    for (int e = 0; e < E / 2; ++e) dst[e] = pack_bf16(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    if (p.lse != nullptr && lane == 0) p.lse[out] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
+        for (int o = 16; o > 0; o >>= 1) l[q] += __shfl_xor_sync(0xffffffffu, l[q], o);
+        if (!real[q]) continue;
+        const float inv = l[q] == 0.f ? 0.f : 1.f / l[q];
+        uint32_t* dst = reinterpret_cast<uint32_t*>(p.O + out[q] * D + lane * E);
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) dst[e] = pack_bf16(acc[q][2 * e] * inv, acc[q][2 * e + 1] * inv);
+        if (p.lse != nullptr && lane == 0) p.lse[out[q]] = l[q] == 0.f ? -INFINITY : (M[q] + log2f(l[q])) * 0.6931471805599453f;
+    }
 }
 
 template <int D, bool HALF>
@@ -395,7 +426,8 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
         const int box = shape->page_size < FEW_KEYS ? shape->page_size : FEW_KEYS;
         const long long rows = (long long)shape->n_pages * shape->page_size;
         CUtensorMap tk, tv;
-        if (!make_tile_map(&tk, K_pages, D, shape->n_kv_heads, rows, box) || !make_tile_map(&tv, V_pages, D, shape->n_kv_heads, rows, box)) return SEKA_ERR_CUDA;
+        if (!make_tile_map(&tk, K_pages, D, shape->n_kv_heads, rows, box, 1, D == 64) ||
+            !make_tile_map(&tv, V_pages, D, shape->n_kv_heads, rows, box, 1, D == 64)) return SEKA_ERR_CUDA;
         const bool half = shape->max_new * G <= 8;
         const unsigned grid = (unsigned)p.n_shares;
         stc = D == 128 ? (half ? launch_few<128, true>(tk, tv, p, grid, st) : launch_few<128, false>(tk, tv, p, grid, st))
@@ -406,7 +438,7 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     }
     if (stc != SEKA_OK || p.n_shares == 1) return stc;
     const int rows = unit_rows(shape);
-    const unsigned grid = (unsigned)(p.n_shares * (rows / MERGE_WARPS));
+    const unsigned grid = (unsigned)(p.n_shares * ((rows + MERGE_WARPS * MERGE_ROWS - 1) / (MERGE_WARPS * MERGE_ROWS)));
     return D == 128 ? launch_kernel(true, paged_merge_kernel<128>, grid, MERGE_WARPS * 32, 0, st, p, rows)
                     : launch_kernel(true, paged_merge_kernel<64>, grid, MERGE_WARPS * 32, 0, st, p, rows);
 }

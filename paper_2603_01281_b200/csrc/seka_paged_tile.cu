@@ -514,8 +514,8 @@ seka_status launch_paged_tiles(const PagedAttnParams& p, const void* Q, const vo
     const int box = page_size < 128 ? page_size : 128;
     const long long rows = (long long)p.v.n_pages * page_size;
     CUtensorMap tq, tk, tv;
-    if (!make_tile_map(&tq, Q, D, p.v.Hq, p.v.T, p.tile_tokens, p.v.G) || !make_tile_map(&tk, K, D, p.v.Hkv, rows, box) ||
-        !make_tile_map(&tv, V, D, p.v.Hkv, rows, box)) return SEKA_ERR_CUDA;
+    if (!make_tile_map(&tq, Q, D, p.v.Hq, p.v.T, p.tile_tokens, p.v.G) || !make_tile_map(&tk, K, D, p.v.Hkv, rows, box, 1, D == 64) ||
+        !make_tile_map(&tv, V, D, p.v.Hkv, rows, box, 1, D == 64)) return SEKA_ERR_CUDA;
     if (cudaFuncSetAttribute(paged_tile_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)G::BYTES) != cudaSuccess) return SEKA_ERR_CUDA;
     return launch_kernel(true, paged_tile_kernel<D>, (unsigned)p.n_shares, NTHREADS, G::BYTES, st, tq, tk, tv, p);
 }
