@@ -80,7 +80,7 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ 
         __syncwarp();
         return ok;
     };
-    Segment sg;
+    Segment sg = {};
     int i = 0;
     bool ok = true;
 
@@ -89,19 +89,15 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ 
         const int bx_shift = p.v.page_shift < 6 ? p.v.page_shift : 6, nb = MF_KEYS >> bx_shift;
         const int box = lane % nb, blk = lane / nb;         // blk >= H: idle
         const uint32_t dst = (uint32_t)(blk * SL::BLOCK_BYTES + (box << bx_shift) * 128);
-        const int pool_rows = p.v.n_pages << p.v.page_shift;
-        auto row_of = [&](int j) -> int {                   // -1: behind the cache.  A page that does not exist reads as zeros
-            const int key = j * MF_KEYS + (box << bx_shift);
-            if (key >= sg.L) return -1;
-            const long long r = load_pool_row(p.v, sg.b, key);
-            return r < 0 ? pool_rows : (int)r;
-        };
+        // first token of this lane's box of stage j; the entry of its page (not looked at where the box lies behind the cache)
+        auto key_of = [&](int j) -> int { return j * MF_KEYS + (box << bx_shift); };
+        auto entry_of = [&](int j) -> int { return key_of(j) < sg.L ? table_entry(p.v, sg.b, key_of(j)) : 0; };
         while (ok && next(sg)) {
-            int row = row_of(sg.j);
+            int entry = entry_of(sg.j);
 #pragma unroll 1
             for (int t = 0; t < sg.n; ++t, ++i) {
                 const int s = i % SL::NSTAGE, round = i / SL::NSTAGE;
-                const int row_next = t + 1 < sg.n ? row_of(sg.j + t + 1) : -1;
+                const int entry_next = t + 1 < sg.n ? entry_of(sg.j + t + 1) : 0, key = key_of(sg.j + t);
                 if (round > 0) {
                     ok = __all_sync(0xffffffffu, mbar_wait(&empty[s], (uint32_t)(round - 1) & 1u, abort_flag, p.v.status, 62));
                     if (!ok) break;
@@ -111,8 +107,8 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ 
                     mbar_expect_tx(&full[s], (uint32_t)(H * min(nb, (keys + (1 << bx_shift) - 1) >> bx_shift) * 128) << bx_shift);
                 }
                 __syncwarp();
-                if (row >= 0 && blk < H) tma_load_3d(smem + s * SL::STAGE_BYTES + dst, &tk, &full[s], blk * 64, sg.h, row);
-                row = row_next;
+                if (key < sg.L && blk < H) tma_load_3d(smem + s * SL::STAGE_BYTES + dst, &tk, &full[s], blk * 64, sg.h, box_row(p.v, entry, key));
+                entry = entry_next;
             }
         }
         __syncwarp();
@@ -204,7 +200,9 @@ struct MtGeo {
     static constexpr uint32_t Q_OFF = 4 * TILE;             // keys: two units of two tiles
     static constexpr uint32_t L_OFF = Q_OFF + NQ * TILE;    // lse (base 2) of the rows of each query tile
     static constexpr uint32_t BAR_OFF = L_OFF + NQ * 512;
-    static constexpr uint32_t NBARS = 4 + 4 * NQ + 8 + 1;
+    // mbarriers, by first index
+    static constexpr uint32_t K_FULL = 0, K_FREE = K_FULL + 2, Q_FULL = K_FREE + 2, Q_FREE = Q_FULL + NQ, L_FULL = Q_FREE + NQ, L_FREE = L_FULL + NQ,
+                              S_FULL = L_FREE + NQ, S_FREE = S_FULL + 4, DRAIN = S_FREE + 4, NBARS = DRAIN + 1;
     static constexpr uint32_t MISC_OFF = BAR_OFF + NBARS * 8, WALK_OFF = (MISC_OFF + 8 + 15) & ~15u;
     static constexpr uint32_t SCRATCH_OFF = WALK_OFF + 12 * 48, BYTES = SCRATCH_OFF + (MT_THREADS / 32 + 4) * 8;
     static_assert(BYTES <= 227 * 1024, "shared memory");
@@ -216,15 +214,16 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     using G = MtGeo<D>;
     constexpr int NQ = G::NQ, NBLK = D / 64;
     extern __shared__ __align__(1024) uint8_t smem[];
-    uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + G::BAR_OFF);     // [2]  both key tiles of a unit landed
-    uint64_t* k_free = k_full + 2;          // [2]      the tensor core is done with them
-    uint64_t* q_full = k_free + 2;          // [NQ]     query tile landed
-    uint64_t* q_free = q_full + NQ;         // [NQ]
-    uint64_t* l_full = q_free + NQ;         // [NQ]     lse of its rows written
-    uint64_t* l_free = l_full + NQ;         // [NQ]     8 summing warps have read it
-    uint64_t* s_full = l_free + NQ;         // [2 x 2]  scores of key tile x, buffer s & 1
-    uint64_t* s_free = s_full + 4;          // [2 x 2]  4 summing warps have them in registers
-    uint64_t* drain = s_free + 4;           // [1]      every product issued has finished
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + G::BAR_OFF);
+    uint64_t* k_full = bars + G::K_FULL;    // [2]      both key tiles of a unit landed
+    uint64_t* k_free = bars + G::K_FREE;          // [2]      the tensor core is done with them
+    uint64_t* q_full = bars + G::Q_FULL;          // [NQ]     query tile landed
+    uint64_t* q_free = bars + G::Q_FREE;         // [NQ]
+    uint64_t* l_full = bars + G::L_FULL;         // [NQ]     lse of its rows written
+    uint64_t* l_free = bars + G::L_FREE;         // [NQ]     8 summing warps have read it
+    uint64_t* s_full = bars + G::S_FULL;         // [2 x 2]  scores of key tile x, buffer s & 1
+    uint64_t* s_free = bars + G::S_FREE;          // [2 x 2]  4 summing warps have them in registers
+    uint64_t* drain = bars + G::DRAIN;           // [1]      every product issued has finished
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + G::MISC_OFF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + G::MISC_OFF + 4);
     long long* scratch = reinterpret_cast<long long*>(smem + G::SCRATCH_OFF);
@@ -281,19 +280,14 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             const int box = lane % nb, blk = lane / nb;     // blk >= NBLK: idle
             const int key_in = box << bx_shift;
             const uint32_t dst = (uint32_t)(key_in >> 7) * G::TILE + (uint32_t)blk * BLK_BYTES + (uint32_t)((key_in & 127) * 128);
-            const int pool_rows = p.v.n_pages << p.v.page_shift;
             const uint32_t q_bytes = (uint32_t)(TP * Gq) * 128u * NBLK;
             auto load_k = [&](const Segment& w, uint32_t n_u) {
                 const int key = w.p * 256 + key_in, keys = w.L - w.p * 256;     // at least one
-                int row = -1;
-                if (key < w.L) {
-                    const long long r = load_pool_row(p.v, w.b, key);
-                    row = r < 0 ? pool_rows : (int)r;       // a page that does not exist reads as zeros
-                }
+                const int entry = key < w.L ? table_entry(p.v, w.b, key) : 0;
                 if (n_u >= 2) { ok = warp_wait(k_free + (n_u & 1), ((n_u >> 1) - 1) & 1, 70); if (!ok) return; }
                 if (leader) mbar_expect_tx(k_full + (n_u & 1), (uint32_t)(min(nb, (keys + (1 << bx_shift) - 1) >> bx_shift) * 128 * NBLK) << bx_shift);
                 __syncwarp();
-                if (row >= 0 && blk < NBLK) tma_load_3d(smem + (n_u & 1) * 2 * G::TILE + dst, &tmK, k_full + (n_u & 1), blk * 64, w.h, row);
+                if (key < w.L && blk < NBLK) tma_load_3d(smem + (n_u & 1) * 2 * G::TILE + dst, &tmK, k_full + (n_u & 1), blk * 64, w.h, box_row(p.v, entry, key));
                 __syncwarp();
             };
             uint32_t loaded_k = 0;          // units whose keys have been asked for

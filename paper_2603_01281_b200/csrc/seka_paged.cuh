@@ -91,6 +91,14 @@ __device__ __forceinline__ PagedSeq load_seq(const PagedView& v, int b) {
     if (!s.valid) report_invalid(v.status, kWhereSeq);
     return s;
 }
+// Row for a TMA box at cached token j, given the entry of its page: a page that does not exist is reported and reads as zeros (the row
+// behind the pool).  Apart from the load of the entry, so that it can be under way while the box before is waited for.
+__device__ __forceinline__ int box_row(const PagedView& v, int entry, int j) {
+    const long long r = pool_row(v, entry, j);
+    if (r >= 0) return (int)r;
+    report_invalid(v.status, kWherePage);
+    return v.n_pages << v.page_shift;
+}
 __device__ __forceinline__ long long load_pool_row(const PagedView& v, int b, int j) {
     const long long r = pool_row(v, table_entry(v, b, j), j);
     if (r < 0) report_invalid(v.status, kWherePage);

@@ -80,29 +80,24 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
         __syncwarp();
         return ok;
     };
-    Segment sg;
+    Segment sg = {};
 
     if (warp == FEW_CONSUMERS) {
         // ------------------------------------------------ producer: a lane per TMA box (K or V, 64 columns, a piece of a page)
         const int bx_shift = p.v.page_shift < 6 ? p.v.page_shift : 6, nb = FEW_KEYS >> bx_shift;
         const int box = lane % nb, blk = (lane / nb) % H, kv = lane / (nb * H);
         const uint32_t dst = (uint32_t)(kv * SL::TILE_BYTES + blk * SL::BLOCK_BYTES + (box << bx_shift) * 128);
-        const int pool_rows = p.v.n_pages << p.v.page_shift;
-        // pool row of this lane's box of stage j; -1: it lies behind the cache.  A page that does not exist reads as zeros.
-        auto row_of = [&](int j) -> int {
-            const int key = j * FEW_KEYS + (box << bx_shift);
-            if (key >= sg.L) return -1;
-            const long long r = load_pool_row(p.v, sg.b, key);
-            return r < 0 ? pool_rows : (int)r;
-        };
+        // first token of this lane's box of stage j; the entry of its page (not looked at where the box lies behind the cache)
+        auto key_of = [&](int j) -> int { return j * FEW_KEYS + (box << bx_shift); };
+        auto entry_of = [&](int j) -> int { return key_of(j) < sg.L ? table_entry(p.v, sg.b, key_of(j)) : 0; };
         int i = 0;
         bool ok = true;
         while (ok && next(sg)) {
-            int row = row_of(sg.j);
+            int entry = entry_of(sg.j);
 #pragma unroll 1
             for (int t = 0; t < sg.n; ++t, ++i) {
                 const int s = i % SL::NSTAGE, round = i / SL::NSTAGE;
-                const int row_next = t + 1 < sg.n ? row_of(sg.j + t + 1) : -1;
+                const int entry_next = t + 1 < sg.n ? entry_of(sg.j + t + 1) : 0, key = key_of(sg.j + t);
                 if (round > 0) {
                     ok = __all_sync(0xffffffffu, mbar_wait(&empty[s], (uint32_t)(round - 1) & 1u, abort_flag, p.v.status, 60));
                     if (!ok) break;
@@ -113,8 +108,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
                     mbar_expect_tx(&full[s], (uint32_t)(2 * H * n_box * 128) << bx_shift);
                 }
                 __syncwarp();
-                if (row >= 0 && kv < 2) tma_load_3d(smem + s * SL::STAGE_BYTES + dst, kv ? &tv : &tk, &full[s], blk * 64, sg.h, row);
-                row = row_next;
+                if (key < sg.L && kv < 2) tma_load_3d(smem + s * SL::STAGE_BYTES + dst, kv ? &tv : &tk, &full[s], blk * 64, sg.h, box_row(p.v, entry, key));
+                entry = entry_next;
             }
         }
         __syncwarp();
