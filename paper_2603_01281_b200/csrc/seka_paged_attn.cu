@@ -404,7 +404,9 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / sqrtf((float)D);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.tile_tokens = few ? shape->max_new : 128 / G;
-    p.geo.tp = few ? shape->max_new : 2 * p.tile_tokens;
+    // one tile of rows at most per sequence and KV head: units of one tile (SHARED tile kernel), else of two.  64 contexts of 2048 on 16 heads
+    // of 64, 17 / 128 new tokens each: 184 / 186 us in units of two, 160 / 164 in units of one; 256 new tokens 228 / 249.
+    p.geo.tp = few ? shape->max_new : shape->max_new <= p.tile_tokens ? p.tile_tokens : 2 * p.tile_tokens;
     p.geo.shift = few ? 6 : 7;
     p.geo.min_share = 4;
     // shares that can have a step, from what the host knows
