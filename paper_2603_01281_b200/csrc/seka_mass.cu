@@ -41,8 +41,8 @@ struct MfSmem {
     static constexpr int NSTAGE = D == 128 ? 6 : 8, CTAS_PER_SM = D == 128 ? 2 : 3;
     static constexpr int STAGE_BYTES = MF_KEYS * D * 2, BLOCK_BYTES = MF_KEYS * 128;
     static constexpr int BAR_OFF = NSTAGE * STAGE_BYTES, WALK_OFF = BAR_OFF + 2 * NSTAGE * 8;
-    static constexpr int SCRATCH_OFF = WALK_OFF + (MF_CONSUMERS + 1) * 48;
-    static constexpr int BYTES = SCRATCH_OFF + (MF_THREADS / 32 + 4) * 8 + 16;
+    static constexpr int BYTES = WALK_OFF + (MF_CONSUMERS + 1) * 48 + 16;
+    static_assert(sizeof(ShareScratch<MF_THREADS>) <= BAR_OFF, "layout");
     static_assert(CTAS_PER_SM * (BYTES + 1024) <= 228 * 1024, "resident CTAs");
 };
 
@@ -54,7 +54,6 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ 
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + SL::BAR_OFF);
     uint64_t* empty = full + SL::NSTAGE;
-    long long* scratch = reinterpret_cast<long long*>(smem + SL::SCRATCH_OFF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SL::BYTES - 16);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -67,7 +66,7 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ 
     pdl_release();
     const int status0 = *reinterpret_cast<volatile int*>(p.v.status);
     if (__syncthreads_or(status0 != 0)) return;
-    const Share share = find_share<MF_THREADS>(p.v, p.key, p.n_shares, (int)blockIdx.x, scratch);
+    const Share share = find_share<MF_THREADS>(p.v, p.key, p.n_shares, (int)blockIdx.x, *reinterpret_cast<ShareScratch<MF_THREADS>*>(smem));
     if (share.len == 0) return;
     Walk* walk = reinterpret_cast<Walk*>(smem + SL::WALK_OFF + warp * 48);
     if (lane == 0) walk_begin(p.v, share, *walk);
@@ -192,6 +191,7 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ 
 constexpr int MT_THREADS = 384;
 constexpr uint32_t BLK_BYTES = 128 * 128;
 constexpr int MT_REGS_CTRL = 104, MT_REGS_SUM = 200;
+constexpr int MT_POLY8 = 2;             // of eight pairs of exponentials, how many run on the multiply-add pipe
 
 template <int D>
 struct MtGeo {
@@ -201,10 +201,11 @@ struct MtGeo {
     static constexpr uint32_t L_OFF = Q_OFF + NQ * TILE;    // lse (base 2) of the rows of each query tile
     static constexpr uint32_t BAR_OFF = L_OFF + NQ * 512;
     // mbarriers, by first index
-    static constexpr uint32_t K_FULL = 0, K_FREE = K_FULL + 2, Q_FULL = K_FREE + 2, Q_FREE = Q_FULL + NQ, L_FULL = Q_FREE + NQ, L_FREE = L_FULL + NQ,
+    static constexpr uint32_t K_FULL = 0, K_FREE = K_FULL + 2, Q_FULL = K_FREE + 2, Q_FREE = Q_FULL + NQ, L_FREE = Q_FREE + NQ,
                               S_FULL = L_FREE + NQ, S_FREE = S_FULL + 4, DRAIN = S_FREE + 4, NBARS = DRAIN + 1;
     static constexpr uint32_t MISC_OFF = BAR_OFF + NBARS * 8, WALK_OFF = (MISC_OFF + 8 + 15) & ~15u;
-    static constexpr uint32_t SCRATCH_OFF = WALK_OFF + 12 * 48, BYTES = SCRATCH_OFF + (MT_THREADS / 32 + 4) * 8;
+    static constexpr uint32_t BYTES = WALK_OFF + 12 * 48;
+    static_assert(sizeof(ShareScratch<MT_THREADS>) <= 4 * TILE, "layout");
     static_assert(BYTES <= 227 * 1024, "shared memory");
 };
 
@@ -219,20 +220,18 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     uint64_t* k_free = bars + G::K_FREE;          // [2]      the tensor core is done with them
     uint64_t* q_full = bars + G::Q_FULL;          // [NQ]     query tile landed
     uint64_t* q_free = bars + G::Q_FREE;         // [NQ]
-    uint64_t* l_full = bars + G::L_FULL;         // [NQ]     lse of its rows written
-    uint64_t* l_free = bars + G::L_FREE;         // [NQ]     8 summing warps have read it
-    uint64_t* s_full = bars + G::S_FULL;         // [2 x 2]  scores of key tile x, buffer s & 1
+    uint64_t* l_free = bars + G::L_FREE;         // [NQ]     8 summing warps have read the lse of its rows
+    uint64_t* s_full = bars + G::S_FULL;         // [2 x 2]  scores of key tile x, buffer s & 1 (the product and the lse of its rows: two arrivals)
     uint64_t* s_free = bars + G::S_FREE;          // [2 x 2]  4 summing warps have them in registers
     uint64_t* drain = bars + G::DRAIN;           // [1]      every product issued has finished
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + G::MISC_OFF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + G::MISC_OFF + 4);
-    long long* scratch = reinterpret_cast<long long*>(smem + G::SCRATCH_OFF);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int Gq = p.v.G, TP = p.rowg.tp;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) { mbar_init(k_full + i, 1); mbar_init(k_free + i, 1); }
-        for (int i = 0; i < NQ; ++i) { mbar_init(q_full + i, 1); mbar_init(q_free + i, 1); mbar_init(l_full + i, 1); mbar_init(l_free + i, 8); }
-        for (int i = 0; i < 4; ++i) { mbar_init(s_full + i, 1); mbar_init(s_free + i, 4); }
+        for (int i = 0; i < NQ; ++i) { mbar_init(q_full + i, 1); mbar_init(q_free + i, 1); mbar_init(l_free + i, 8); }
+        for (int i = 0; i < 4; ++i) { mbar_init(s_full + i, 2); mbar_init(s_free + i, 4); }
         mbar_init(drain, 1);
         *abort_flag = 0;
         mbar_fence_init();
@@ -245,7 +244,7 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     pdl_wait();
     const int status0 = *reinterpret_cast<volatile int*>(p.v.status);
     if (__syncthreads_or(status0 != 0)) return;
-    const Share share = find_share<MT_THREADS>(p.v, p.rowg, p.n_shares, (int)blockIdx.x, scratch);
+    const Share share = find_share<MT_THREADS>(p.v, p.rowg, p.n_shares, (int)blockIdx.x, *reinterpret_cast<ShareScratch<MT_THREADS>*>(smem));
     if (tid == 0) write_cut(p.cuts, p.v, p.rowg, share, (int)blockIdx.x);
     if (share.len == 0) return;
     if (warp == 0) { tmem_alloc(tmem_holder, 512); tmem_relinquish(); }
@@ -373,11 +372,14 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     for (int i = 0; i < 4; ++i)
                         l[i] = tt[i] < TP && tok0 + tt[i] < it.n_new ? p.lse[(size_t)(it.q0 + tok0 + tt[i]) * p.v.Hq + (size_t)it.h * Gq + g[i]] * kLog2e : INFINITY;
                     if (s >= NQ) { ok = warp_wait(l_free + s % NQ, (s / NQ - 1) & 1, 75); if (!ok) break; }
+                    // one arrival per phase: the scores that used the buffers before are complete
+                    for (int x = 0; x < 2 && ok && s >= 2; ++x) ok = warp_wait(s_full + 2 * x + (s & 1), ((s >> 1) - 1) & 1, 78);
+                    if (!ok) break;
                     float* dst = reinterpret_cast<float*>(smem + G::L_OFF + (s % NQ) * 512);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) dst[i * 32 + lane] = -l[i];
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(l_full + s % NQ);
+                    if (lane == 0) { mbar_arrive(s_full + (s & 1)); mbar_arrive(s_full + 2 + (s & 1)); }
                 }
             }
         }
@@ -390,45 +392,64 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         while (ok && next(it)) {
             const int key = it.p * 256 + x * 128 + row, t0 = p.rowg.first(it.L, it.n_new, it.p) + it.j;
             float2 sum[4] = {};
+            // 32 columns at a time; the next 32 (at the end of a step the next step's first) are on their way from tensor memory meanwhile,
+            // so that the special-function unit does not run dry
+            uint32_t v[2][32];
+            ok = warp_wait(s_full + 2 * x + (s & 1), (s >> 1) & 1, 76 + x);
+            if (!ok) break;
+            tc_fence_after();
+            tmem_ld32(tS + (s & 1) * 128, v[0]);
+            tmem_wait_ld_on(v[0]);
 #pragma unroll 1
             for (int j = 0; j < it.n; ++j, ++s) {
                 const int tok0 = (t0 + j) * TP;
                 // columns [c_lo, c_hi) are rows of tokens that exist and see this thread's cached token
                 const int d = key - it.old - tok0;
                 const int c_lo = d <= 0 ? 0 : d >= TP ? 128 : d * Gq, c_hi = min(TP, it.n_new - tok0) * Gq;
-                ok = warp_wait(s_full + 2 * x + (s & 1), (s >> 1) & 1, 76 + x);
-                if (ok) ok = warp_wait(l_full + s % NQ, (s / NQ) & 1, 78);
-                if (!ok) break;
-                tc_fence_after();
-                uint32_t v[128];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32(tS + (s & 1) * 128 + c * 32, reinterpret_cast<uint32_t(&)[32]>(v[32 * c]));
-                tmem_wait_ld();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(s_free + 2 * x + (s & 1));
-                const float4* nl = reinterpret_cast<const float4*>(smem + G::L_OFF + (s % NQ) * 512);
                 const bool part = __any_sync(0xffffffffu, c_lo > 0 || c_hi < TP * Gq);
-                if (!part) {
+                bool there = true;              // the next step's scores (asked for a while before they are needed)
+                const float4* nl = reinterpret_cast<const float4*>(smem + G::L_OFF + (s % NQ) * 512);
 #pragma unroll
-                    for (int e = 0; e < 128; e += 4) {
-                        const float4 n = nl[e / 4];
-                        const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), sc2, make_float2(n.x, n.y));
-                        const float2 b = __ffma2_rn(make_float2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), sc2, make_float2(n.z, n.w));
-                        sum[(e / 2) & 3] = __fadd2_rn(sum[(e / 2) & 3], make_float2(fast_exp2(a.x), fast_exp2(a.y)));
-                        sum[(e / 2 + 1) & 3] = __fadd2_rn(sum[(e / 2 + 1) & 3], make_float2(fast_exp2(b.x), fast_exp2(b.y)));
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t (&cur)[32] = v[c & 1];
+                    if (c < 3) {
+                        tmem_ld32(tS + (s & 1) * 128 + (c + 1) * 32, v[(c + 1) & 1]);
+                        if (c == 2 && j + 1 < it.n) there = mbar_try_wait(s_full + 2 * x + ((s + 1) & 1), ((s + 1) >> 1) & 1);
+                    } else if (j + 1 < it.n) {
+                        if (!__all_sync(0xffffffffu, there)) ok = warp_wait(s_full + 2 * x + ((s + 1) & 1), ((s + 1) >> 1) & 1, 76 + x);
+                        if (!ok) break;
+                        tc_fence_after();
+                        tmem_ld32(tS + ((s + 1) & 1) * 128, v[0]);
                     }
-                } else {
+                    if (!part) {
 #pragma unroll
-                    for (int e = 0; e < 128; e += 4) {
-                        const float4 n = nl[e / 4];
-                        auto w = [&](int i, float m) -> float {
-                            return e + i >= c_lo && e + i < c_hi ? fast_exp2(fmaf(__uint_as_float(v[e + i]), p.scale_log2, m)) : 0.f;
-                        };
-                        sum[(e / 2) & 3] = __fadd2_rn(sum[(e / 2) & 3], make_float2(w(0, n.x), w(1, n.y)));
-                        sum[(e / 2 + 1) & 3] = __fadd2_rn(sum[(e / 2 + 1) & 3], make_float2(w(2, n.z), w(3, n.w)));
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 n = nl[8 * c + e / 4];
+                            const float2 a = __ffma2_rn(make_float2(__uint_as_float(cur[e]), __uint_as_float(cur[e + 1])), sc2, make_float2(n.x, n.y));
+                            const float2 b = __ffma2_rn(make_float2(__uint_as_float(cur[e + 2]), __uint_as_float(cur[e + 3])), sc2, make_float2(n.z, n.w));
+                            auto pw = [](float2 w, int pair) { return (pair & 7) < MT_POLY8 ? exp2_poly2(w) : make_float2(fast_exp2(w.x), fast_exp2(w.y)); };
+                            sum[(e / 2) & 3] = __fadd2_rn(sum[(e / 2) & 3], pw(a, 3 * (e / 2)));
+                            sum[(e / 2 + 1) & 3] = __fadd2_rn(sum[(e / 2 + 1) & 3], pw(b, 3 * (e / 2 + 1)));
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 n = nl[8 * c + e / 4];
+                            auto w = [&](int i, float m) -> float {
+                                return 32 * c + e + i >= c_lo && 32 * c + e + i < c_hi ? fast_exp2(fmaf(__uint_as_float(cur[e + i]), p.scale_log2, m)) : 0.f;
+                            };
+                            sum[(e / 2) & 3] = __fadd2_rn(sum[(e / 2) & 3], make_float2(w(0, n.x), w(1, n.y)));
+                            sum[(e / 2 + 1) & 3] = __fadd2_rn(sum[(e / 2 + 1) & 3], make_float2(w(2, n.z), w(3, n.w)));
+                        }
+                    }
+                    tmem_wait_ld_on(v[(c + 1) & 1]);
+                    if (c == 2) {                           // all scores of the step are in registers
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(s_free + 2 * x + (s & 1));
                     }
                 }
+                if (!ok) break;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(l_free + s % NQ);
             }
@@ -513,8 +534,8 @@ extern "C" seka_status seka_attention_mass(const seka_paged_shape* shape, const 
     p.Q = static_cast<const __nv_bfloat16*>(Q); p.lse = lse; p.mass_in = mass_in; p.mass_out = mass_out;
     const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / sqrtf((float)D);
     p.scale_log2 = scale * kLog2e;
-    p.key = KeyGeo{6, 4};
-    p.rowg = RowGeo{128 / G, 8, 2};
+    p.key = KeyGeo{6, 4, 1};
+    p.rowg = RowGeo{128 / G, 8, 2, (p.v.cap + 255) / 256};
     p.cuts = reinterpret_cast<CutRecord*>(ws + w.cut_off);
     p.part = reinterpret_cast<float*>(ws + w.mass_part_off);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -29,9 +29,8 @@ struct FewSmem {
     static constexpr int MERGE_OFF = NSTAGE * STAGE_BYTES;          // [4 warps][8 rows]
     static constexpr int BAR_OFF = MERGE_OFF + FEW_CONSUMERS * 8 * MERGE_STRIDE * 4;
     static constexpr int WALK_OFF = BAR_OFF + 2 * NSTAGE * 8;
-    static constexpr int SCRATCH_OFF = WALK_OFF + (FEW_CONSUMERS + 1) * 48;
-    static constexpr int BYTES = SCRATCH_OFF + (FEW_THREADS / 32 + 4) * 8 + 16;
-    static_assert(BAR_OFF % 8 == 0 && WALK_OFF % 16 == 0 && SCRATCH_OFF % 8 == 0, "alignment");
+    static constexpr int BYTES = WALK_OFF + (FEW_CONSUMERS + 1) * 48 + 16;
+    static_assert(BAR_OFF % 8 == 0 && WALK_OFF % 16 == 0 && sizeof(ShareScratch<FEW_THREADS>) <= BAR_OFF, "layout");
     static_assert(CTAS_PER_SM * (BYTES + 1024) <= 228 * 1024, "resident CTAs");
 };
 
@@ -52,7 +51,6 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + SL::BAR_OFF);
     uint64_t* empty = full + SL::NSTAGE;
-    long long* scratch = reinterpret_cast<long long*>(smem + SL::SCRATCH_OFF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SL::BYTES - 16);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -66,7 +64,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
     pdl_release();
     const int status0 = *reinterpret_cast<volatile int*>(p.v.status);
     if (__syncthreads_or(status0 != 0)) return;             // an earlier launch gave up on this workspace
-    const Share share = find_share<FEW_THREADS>(p.v, p.geo, p.n_shares, (int)blockIdx.x, scratch);
+    const Share share = find_share<FEW_THREADS>(p.v, p.geo, p.n_shares, (int)blockIdx.x, *reinterpret_cast<ShareScratch<FEW_THREADS>*>(smem));
     if (tid == 0) write_cut(p.cuts, p.v, p.geo, share, (int)blockIdx.x);
     if (share.len == 0) return;
     Walk* walk = reinterpret_cast<Walk*>(smem + SL::WALK_OFF + warp * 48);
@@ -409,6 +407,7 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     p.geo.tp = few ? shape->max_new : shape->max_new <= p.tile_tokens ? p.tile_tokens : 2 * p.tile_tokens;
     p.geo.shift = few ? 6 : 7;
     p.geo.min_share = 4;
+    p.geo.max_units = (shape->max_new + p.geo.tp - 1) / p.geo.tp;
     // shares that can have a step, from what the host knows
     const long long units = few ? shape->batch : (long long)shape->total_new / p.geo.tp + shape->batch;
     const long long steps = units * shape->n_kv_heads * ((p.v.cap + (1 << p.geo.shift) - 1) >> p.geo.shift);

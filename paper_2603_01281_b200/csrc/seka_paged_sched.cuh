@@ -7,32 +7,19 @@
 // itself and finds where its share begins.  What a unit and a step are is the geometry's to say:
 //   units(L, n)      units of a sequence with L cached tokens, the last n of them new, per KV head
 //   steps(L, n, u)   steps of its unit u (at least 1)
-//   prefix(L, n, u)  steps of its first u units
+//   max_units        no sequence has more units (from what the host knows)
 #pragma once
 
 #include "seka_paged.cuh"
 
 namespace seka {
 
-// sum of floor((a i + b) / m) over 0 <= i < n, all non-negative, m > 0 (Euclid's algorithm on the lattice points below the line)
-SEKA_HD unsigned long long floor_sum(unsigned long long n, unsigned long long m, unsigned long long a, unsigned long long b) {
-    unsigned long long ans = 0;
-    while (n > 0) {
-        if (a >= m) { ans += n * (n - 1) / 2 * (a / m); a %= m; }
-        if (b >= m) { ans += n * (b / m); b %= m; }
-        const unsigned long long y = a * n + b;
-        if (y < m) break;
-        n = y / m; b = y % m;
-        const unsigned long long t = m; m = a; a = t;
-    }
-    return ans;
-}
-
 // Attention: the queries of `tp` consecutive new tokens (with their whole query group); a step is a tile of 2^shift cached tokens, up
 // to the last one that the unit's last token sees (a unit that sees none has one step, all masked).
 struct StepGeo {
     int tp, shift;
     int min_share;      // steps that a share has at least
+    int max_units;
     SEKA_HD int steps_to(int L, int n, int last) const {
         const int x = L - n + last;
         return x <= (1 << shift) ? 1 : (int)(((long long)x + (1 << shift) - 1) >> shift);
@@ -42,71 +29,35 @@ struct StepGeo {
         const int last = (p + 1) * tp;
         return steps_to(L, n, last < n ? last : n);
     }
-    SEKA_HD long long prefix(int L, int n, int u) const {
-        if (u <= 0) return 0;
-        const int U = units(L, n), old = L - n;
-        long long s = 0;
-        const int full = u < U ? u : U - 1;     // units of exactly tp tokens
-        int p = 0;
-        while (p < full && (long long)old + (long long)(p + 1) * tp < 1) { ++s; ++p; }      // padding: units without a key
-        if (p < full)
-            s += (long long)floor_sum((unsigned long long)(full - p), 1ull << shift, (unsigned long long)tp,
-                                      (unsigned long long)((long long)old + (long long)(p + 1) * tp + (1 << shift) - 1));
-        if (u >= U) s += steps(L, n, U - 1);
-        return s;
-    }
 };
 
 // Accumulated weights, few rows: all cached tokens of a sequence; a step is 2^shift of them.
 struct KeyGeo {
-    int shift, min_share;
+    int shift, min_share, max_units;
     SEKA_HD int units(int L, int) const { return L > 0 ? 1 : 0; }
     SEKA_HD int steps(int L, int, int) const { return (int)(((long long)L + (1 << shift) - 1) >> shift); }
-    SEKA_HD long long prefix(int L, int n, int u) const { return u > 0 ? steps(L, n, 0) : 0; }
 };
 
 // Accumulated weights, many rows: 2^shift cached tokens; a step is the queries of `tp` new tokens, from the first that sees any of
 // them (a sequence without new tokens has one empty step).
 struct RowGeo {
-    int tp, shift, min_share;
+    int tp, shift, min_share, max_units;
     SEKA_HD int tiles(int n) const { return n > 0 ? (n + tp - 1) / tp : 1; }
     SEKA_HD int first(int L, int n, int u) const {
         const long long x = ((long long)u << shift) - (L - n);
-        return x > 0 ? (int)(x / tp) : 0;
+        return x > 0 ? (int)((uint32_t)x / (uint32_t)tp) : 0;       // (keys and tokens are counted in 31 bits)
     }
     SEKA_HD int units(int L, int) const { return (int)(((long long)L + (1 << shift) - 1) >> shift); }
     SEKA_HD int steps(int L, int n, int u) const { return tiles(n) - first(L, n, u); }
-    SEKA_HD long long prefix(int L, int n, int u) const {
-        const long long old = L - n, k0 = old <= 0 ? 0 : (old + (1 << shift) - 1) >> shift;
-        long long s = (long long)tiles(n) * u;
-        if (u > k0) s -= (long long)floor_sum((unsigned long long)(u - k0), (unsigned long long)tp, 1ull << shift, (unsigned long long)((k0 << shift) - old));
-        return s;
-    }
 };
 
 // A place on the line: step `j` of unit p of KV head h of sequence b.
 struct LinePos { int b, h, p, j; };
 
-// `r` steps into the sequence b (0 <= r < Hkv * steps of a head)
-template <typename Geo> SEKA_HD LinePos place_in_seq(const Geo& g, int b, int L, int n, long long per_head, long long r) {
-    LinePos c;
-    c.b = b; c.h = (int)(r / per_head);
-    r -= c.h * per_head;
-    int lo = 0, hi = g.units(L, n) - 1;                 // largest p with prefix(p) <= r
-    while (lo < hi) {
-        const int mid = lo + (hi - lo + 1) / 2;
-        if (g.prefix(L, n, mid) <= r) lo = mid; else hi = mid - 1;
-    }
-    c.p = lo; c.j = (int)(r - g.prefix(L, n, lo));
-    return c;
-}
-
 // What the merge needs of the cut where a share begins: the unit it falls into (n: its steps; 0: the share is empty).
 struct CutRecord { int b, h, p, j, n, share; };
 
 #ifdef __CUDACC__
-
-constexpr long long kNoPlace = -1;
 
 struct Share {
     long long len;          // steps of this CTA
@@ -114,66 +65,105 @@ struct Share {
     int share;              // steps of a full share
 };
 
-// Every thread of a block of NT calls; the block's share of the line among `n_cta`.  `scratch`: NT / 32 + 4 words of 8 bytes.
-template <int NT, typename Geo>
-__device__ inline Share find_share(const PagedView& v, const Geo& g, int n_cta, int cta, long long* scratch) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int NW = NT / 32;
-    // steps of the sequences, a block's worth at a time; with up to NT sequences they stay in a register
-    long long mine = 0;
-    int L = 0, n = 0;
-    auto steps_of = [&](int b) -> long long {
-        if (b >= v.B) { n = 0; L = 0; return 0; }
-        const PagedSeq s = load_seq(v, b);
-        n = s.n; L = s.L;
-        return g.prefix(L, n, g.units(L, n)) * v.Hkv;
-    };
-    long long total = 0;
-    for (int b0 = 0; b0 < v.B; b0 += NT) { mine = steps_of(b0 + tid); total += mine; }
+// What find_share needs of shared memory, before anything else is in it.
+template <int NT> struct ShareScratch {
+    long long warp_sum[NT / 32];
+    long long rest;                     // steps into the KV head that the share begins in
+    int b, L, n, h, p, j;
+    int len[NT], new_tokens[NT], steps[NT];
+};
+
+// exclusive scan over the block; `all` receives the sum
+template <int NT> __device__ __forceinline__ long long block_scan(long long x, long long* warp_sum, long long& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long inc = x;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    if (lane == 0) scratch[warp] = total;
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    __syncthreads();                    // the sums of the scan before have been read
+    if (lane == 31) warp_sum[warp] = inc;
     __syncthreads();
-    total = 0;
+    long long before = 0;
+    all = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) total += scratch[w];
-    long long share = (total + n_cta - 1) / n_cta;
+    for (int w = 0; w < NT / 32; ++w) {
+        if (w < warp) before += warp_sum[w];
+        all += warp_sum[w];
+    }
+    return before + inc - x;
+}
+
+// Every thread of a block of NT calls: the block's share of the line among `n_cta`.  Sequences by thread, NT at a time, then the units of
+// the one that the share begins in; the steps of a sequence of many units are added up by a warp.  (In closed form, sums of floors by
+// Euclid's algorithm, the 64-bit divisions and a binary search over them took 10 us.)
+template <int NT, typename Geo>
+__device__ inline Share find_share(const PagedView& v, const Geo& g, int n_cta, int cta, ShareScratch<NT>& sc) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    long long mine = 0;                 // steps of this thread's sequence; with up to NT sequences it stays in a register
+    int L = 0, n = 0;
+    auto count = [&](int b0) {
+        const int b = b0 + tid;
+        L = 0; n = 0;
+        if (b < v.B) { const PagedSeq s = load_seq(v, b); L = s.L; n = s.n; }
+        int per = 0;
+        if (g.max_units <= 8) {
+            const int U = b < v.B ? g.units(L, n) : 0;
+            for (int u = 0; u < U; ++u) per += g.steps(L, n, u);
+        } else {
+            sc.len[tid] = L; sc.new_tokens[tid] = n;
+            __syncthreads();
+            for (int k = warp; k < NT && b0 + k < v.B; k += NT / 32) {
+                const int Lk = sc.len[k], nk = sc.new_tokens[k], U = g.units(Lk, nk);
+                int t = 0;
+                for (int u = lane; u < U; u += 32) t += g.steps(Lk, nk, u);
+                t = __reduce_add_sync(0xffffffffu, t);
+                if (lane == 0) sc.steps[k] = t;
+            }
+            __syncthreads();
+            if (b < v.B) per = sc.steps[tid];
+        }
+        mine = (long long)per * v.Hkv;
+    };
+    long long total = 0, all;
+    for (int b0 = 0; b0 < v.B; b0 += NT) { count(b0); total += mine; }
+    block_scan<NT>(total, sc.warp_sum, all);
+    long long share = (all + n_cta - 1) / n_cta;
     if (share < g.min_share) share = g.min_share;
     Share r;
     r.share = (int)share;
     const long long x = share * cta;
-    r.len = total - x < share ? total - x : share;
+    r.len = all - x < share ? all - x : share;
     r.at = LinePos{0, 0, 0, 0};
-    if (r.len <= 0) { r.len = 0; return r; }            // (uniform)
-    int* place = reinterpret_cast<int*>(scratch + NW);
+    if (r.len <= 0) { r.len = 0; return r; }            // (the same for the whole block)
     long long before = 0;
     for (int b0 = 0; b0 < v.B; b0 += NT) {
-        if (v.B > NT) mine = steps_of(b0 + tid);
-        long long inc = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += y;
-        }
-        __syncthreads();
-        if (lane == 31) scratch[warp] = inc;
-        __syncthreads();
-        long long mybase = before, all = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            if (w < warp) mybase += scratch[w];
-            all += scratch[w];
-        }
-        mybase += inc - mine;
-        if (mine > 0 && x >= mybase && x < mybase + mine) {
-            const LinePos c = place_in_seq(g, b0 + tid, L, n, mine / v.Hkv, x - mybase);
-            place[0] = c.b; place[1] = c.h; place[2] = c.p; place[3] = c.j;
+        if (v.B > NT) count(b0);
+        const long long at = before + block_scan<NT>(mine, sc.warp_sum, all);
+        if (mine > 0 && x >= at && x < at + mine) {
+            sc.b = b0 + tid; sc.L = L; sc.n = n;
+            const long long per = mine / v.Hkv;
+            sc.h = (int)((x - at) / per);
+            sc.rest = x - at - sc.h * per;
         }
         before += all;
-        if (before > x) break;                          // (uniform)
+        if (before > x) break;                          // (the same for the whole block)
     }
     __syncthreads();
-    r.at = LinePos{place[0], place[1], place[2], place[3]};
+    const int U = g.units(sc.L, sc.n);
+    before = 0;
+    for (int u0 = 0; u0 < U; u0 += NT) {
+        const int st = u0 + tid < U ? g.steps(sc.L, sc.n, u0 + tid) : 0;
+        const long long at = before + block_scan<NT>(st, sc.warp_sum, all);
+        if (sc.rest >= at && sc.rest < at + st) { sc.p = u0 + tid; sc.j = (int)(sc.rest - at); }
+        before += all;
+        if (before > sc.rest) break;
+    }
+    __syncthreads();
+    r.at = LinePos{sc.b, sc.h, sc.p, sc.j};
+    fence_proxy_async();                // the scratch lies where copies will land
+    __syncthreads();
     return r;
 }
 

@@ -45,10 +45,9 @@ struct TGeo {
     static constexpr uint32_t Q_FULL = 0, K0_FULL = Q_FULL + 2, KV_FULL = K0_FULL + 1, KV_FREE = KV_FULL + NK, S_FULL = KV_FREE + NK, P_FULL = S_FULL + 2,
                               P_LAST = P_FULL + 2, O_FULL = P_LAST + 2, O_DRAINED = O_FULL + 2, START_FULL = O_DRAINED + 2, DRAIN = START_FULL + 1,
                               HALF_READY = DRAIN + 1, O_STEP = HALF_READY + 1, SEG_FULL = O_STEP + 2, SEG_FREE = SEG_FULL + NSEG, NBARS = SEG_FREE + NSEG;
-    static constexpr uint32_t MISC_OFF = BAR_OFF + NBARS * 8, SEG_OFF = (MISC_OFF + 16 + 15) & ~15u, SCRATCH_OFF = SEG_OFF + NSEG * 48;
-    static constexpr uint32_t STATE_OFF = SCRATCH_OFF + (NTHREADS / 32 + 4) * 8;       // (SHARED) maximum and sum of B's half, a row each
+    static constexpr uint32_t MISC_OFF = BAR_OFF + NBARS * 8, SEG_OFF = (MISC_OFF + 16 + 15) & ~15u, STATE_OFF = SEG_OFF + NSEG * 48;       // (SHARED) maximum and sum of B's half, a row each
     static constexpr uint32_t BYTES = STATE_OFF + 128 * 8;
-    static_assert(MISC_OFF % 8 == 0 && SCRATCH_OFF % 8 == 0, "alignment");
+    static_assert(MISC_OFF % 8 == 0 && STATE_OFF % 8 == 0 && sizeof(ShareScratch<NTHREADS>) <= BAR_OFF, "layout");
     static_assert(BYTES <= 227 * 1024, "shared memory");
 };
 
@@ -101,7 +100,6 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint64_t* seg_free = bars + G::SEG_FREE; // [NSEG] 11 warps have read it
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + G::MISC_OFF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + G::MISC_OFF + 4);
-    long long* scratch = reinterpret_cast<long long*>(smem + G::SCRATCH_OFF);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         mbar_init(q_full + 0, 1); mbar_init(q_full + 1, 1); mbar_init(k0_full, 1);
@@ -119,7 +117,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     pdl_wait();
     const int status0 = *reinterpret_cast<volatile int*>(p.v.status), hook_skip = p.v.status[4], limit_us = p.v.status[5];
     if (__syncthreads_or(status0 != 0)) return;              // an earlier launch gave up on this workspace
-    const Share share = find_share<NTHREADS>(p.v, p.geo, p.n_shares, (int)blockIdx.x, scratch);
+    const Share share = find_share<NTHREADS>(p.v, p.geo, p.n_shares, (int)blockIdx.x, *reinterpret_cast<ShareScratch<NTHREADS>*>(smem));
     if (tid == 0) write_cut(p.cuts, p.v, p.geo, share, (int)blockIdx.x);
     if (share.len == 0) return;
     if (warp == 0) { tmem_alloc(tmem_holder, TMEM_COLS); tmem_relinquish(); }
