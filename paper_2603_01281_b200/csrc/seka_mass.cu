@@ -406,7 +406,8 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 // columns [c_lo, c_hi) are rows of tokens that exist and see this thread's cached token
                 const int d = key - it.old - tok0;
                 const int c_lo = d <= 0 ? 0 : d >= TP ? 128 : d * Gq, c_hi = min(TP, it.n_new - tok0) * Gq;
-                const bool part = __any_sync(0xffffffffu, c_lo > 0 || c_hi < TP * Gq);
+                // of all columns of all rows of the warp: none masked, or none left
+                const bool clean = !__any_sync(0xffffffffu, c_lo > 0 || c_hi < TP * Gq), none = !__any_sync(0xffffffffu, c_lo < c_hi);
                 bool there = true;              // the next step's scores (asked for a while before they are needed)
                 const float4* nl = reinterpret_cast<const float4*>(smem + G::L_OFF + (s % NQ) * 512);
 #pragma unroll
@@ -421,7 +422,7 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                         tc_fence_after();
                         tmem_ld32(tS + ((s + 1) & 1) * 128, v[0]);
                     }
-                    if (!part) {
+                    if (clean) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
                             const float4 n = nl[8 * c + e / 4];
@@ -431,7 +432,7 @@ mass_tile_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                             sum[(e / 2) & 3] = __fadd2_rn(sum[(e / 2) & 3], pw(a, 3 * (e / 2)));
                             sum[(e / 2 + 1) & 3] = __fadd2_rn(sum[(e / 2 + 1) & 3], pw(b, 3 * (e / 2 + 1)));
                         }
-                    } else {
+                    } else if (!none) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
                             const float4 n = nl[8 * c + e / 4];
