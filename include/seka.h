@@ -254,7 +254,7 @@ seka_status seka_learn_projections(const seka_learn_shape* shape, const void* h,
  *    exist: such a token is padding (nothing is stored for it, it sees no key).  A padded decode batch has cache_lens[b] = 0
  *    for the idle sequences.
  *  - Per-row state of the cache (accumulated weight, position) is [B, Hkv, cap], a row per cached token and KV head.  Rows
- *    behind cache_lens[b] are never read or written.
+ *    behind cache_lens[b] are never used and never written.  These arrays are 16-byte aligned.
  *  - One workspace of seka_paged_workspace_bytes(shape) bytes serves all calls, 256-byte aligned, first 256 bytes the status block.  A
  *    length, token offset or page number outside its range, found on the device, records SEKA_ERR_INVALID_ARG there; nothing outside
  *    the buffers is touched, the call's outputs are then undefined.  A launch on a workspace whose status is not SEKA_OK does nothing.

@@ -272,7 +272,7 @@ def test_evict(lens, Hkv, d, page, keep, recent, share, kind):
 
 def test_evict_long_rows_and_many_pairs():
     # one sequence whose ranks do not fit in a CTA's shared memory, in a batch that leaves each pair one CTA
-    c = R.Cache([42000] + [20] * 37, [0] * 38, 4, 4, 64, 256, seed=12)
+    c = R.Cache([44000] + [20] * 37, [0] * 38, 4, 4, 64, 256, seed=12)
     m = torch.randn((c.B, 4, c.cap), generator=c.g).mul(1.5).exp().cuda()
     pos = torch.arange(c.cap, dtype=torch.int32).expand(c.B, 4, -1).contiguous().cuda()
     protect = (torch.rand((c.B, 30000), generator=c.g) < 0.2).to(torch.uint8).cuda()
