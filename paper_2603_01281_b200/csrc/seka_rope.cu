@@ -70,6 +70,35 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopePar
     if (tid < ROPE_TOKENS) { tok[tid][0] = -1; tok[tid][1] = -1; tok[tid][2] = -1; }
     __syncthreads();
     if (status0 != 0) return;
+    const int Hq = p.v.Hq, Hkv = p.v.Hkv, n_rows = Hq + 2 * Hkv, groups = (n_rows + RPW - 1) / RPW;
+    const int sub = lane / LPR, q = lane % LPR;
+    // the lane's two runs of eight elements: pair i is (x[i], x[8 + i]) (HALVES) or (x[2 i], x[2 i + 1]) of them
+    const bool apart = MODE == HALVES && 16 * q < r;
+    const int e0 = apart ? 8 * q : 16 * q, e1 = apart ? half + 8 * q : 16 * q + 8;
+    struct Row { int i, h; bool have; };                    // token, head (queries, keys, values one after another)
+    auto row_of = [&](int k) -> Row {
+        Row w;
+        w.i = k / groups;
+        w.h = (k - w.i * groups) * RPW + sub;
+        w.have = w.i < nt && w.h < n_rows;
+        return w;
+    };
+    auto load = [&](const Row& w, float (&x)[16]) {
+        if (!w.have) return;
+        const size_t t = (size_t)(t0 + w.i);
+        const T* src = w.h < Hq ? static_cast<const T*>(p.Q) + t * p.q_stride + (size_t)w.h * D
+                     : w.h < Hq + Hkv ? static_cast<const T*>(p.K) + t * p.k_stride + (size_t)(w.h - Hq) * D
+                                      : static_cast<const T*>(p.V) + t * p.v_stride + (size_t)(w.h - Hq - Hkv) * D;
+        load8(src + e0, x, 0);
+        load8(src + e1, x, 8);
+    };
+    // the first rows are on their way while the tokens' sequences, pages and angles are found
+    const int step = ROPE_WARPS * (int)gridDim.y;
+    int k = (int)blockIdx.y * ROPE_WARPS + warp;
+    Row wa = row_of(k), wb = row_of(k + step);
+    float xa[16], xb[16];
+    load(wa, xa);
+    load(wb, xb);
     // the sequences that own the tokens
     for (int b = tid; b < p.v.B; b += ROPE_THREADS) {
         const int q0 = p.v.cu ? p.v.cu[b] : b * p.v.max_new, q1 = p.v.cu ? p.v.cu[b + 1] : q0 + p.v.max_new;
@@ -93,35 +122,12 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopePar
         cs[i][k] = make_float2(c * p.magnitude, sn * p.magnitude);
     }
     __syncthreads();
-    const int Hq = p.v.Hq, Hkv = p.v.Hkv, n_rows = Hq + 2 * Hkv, groups = (n_rows + RPW - 1) / RPW;
-    const int sub = lane / LPR, q = lane % LPR;
-    // the lane's two runs of eight elements: pair i is (x[i], x[8 + i]) (HALVES) or (x[2 i], x[2 i + 1]) of them
-    const bool apart = MODE == HALVES && 16 * q < r;
-    const int e0 = apart ? 8 * q : 16 * q, e1 = apart ? half + 8 * q : 16 * q + 8;
-    struct Row { int i, h; long long row; bool have, turn; };
-    auto row_of = [&](int k) -> Row {
-        Row w;
-        w.i = k / groups;
-        w.h = (k - w.i * groups) * RPW + sub;
-        w.row = w.i < nt ? (long long)tok[w.i][2] : -1;
-        w.have = w.i < nt && w.h < n_rows && (w.h < Hq || w.row >= 0);
-        w.turn = w.have && w.h < Hq + Hkv;
-        return w;
-    };
-    auto load = [&](const Row& w, float (&x)[16]) {
-        if (!w.have) return;
-        const size_t t = (size_t)(t0 + w.i);
-        const T* src = w.h < Hq ? static_cast<const T*>(p.Q) + t * p.q_stride + (size_t)w.h * D
-                     : w.h < Hq + Hkv ? static_cast<const T*>(p.K) + t * p.k_stride + (size_t)(w.h - Hq) * D
-                                      : static_cast<const T*>(p.V) + t * p.v_stride + (size_t)(w.h - Hq - Hkv) * D;
-        load8(src + e0, x, 0);
-        load8(src + e1, x, 8);
-    };
     auto finish = [&](const Row& w, float (&x)[16]) {
+        const bool turn = w.have && w.h < Hq + Hkv;
         if (MODE == STAGED) {
             T* mine = stage[warp][sub];
             __syncwarp();                                   // the rows before have been read
-            if (w.turn) {
+            if (turn) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 8) {
                     if constexpr (sizeof(T) == 2) store8(mine + e0 + i, x, i);
@@ -143,8 +149,8 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopePar
                 }
             }
             __syncwarp();
-            if (w.turn) { load8(mine + e0, x, 0); load8(mine + e1, x, 8); }
-        } else if (w.turn && 16 * q < r) {
+            if (turn) { load8(mine + e0, x, 0); load8(mine + e1, x, 8); }
+        } else if (turn && 16 * q < r) {
             const float4* c4 = reinterpret_cast<const float4*>(&cs[w.i][8 * q]);
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
@@ -160,20 +166,22 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopePar
             }
         }
         if (!w.have) return;
+        const long long row = tok[w.i][2];
+        if (w.h >= Hq && row < 0) return;                   // padding, or no such page
         __nv_bfloat16* dst = w.h < Hq ? p.Q_out + ((size_t)(t0 + w.i) * Hq + w.h) * D
-                           : w.h < Hq + Hkv ? p.K_pages + ((size_t)w.row * Hkv + (w.h - Hq)) * D
-                                            : p.V_pages + ((size_t)w.row * Hkv + (w.h - Hq - Hkv)) * D;
+                           : w.h < Hq + Hkv ? p.K_pages + ((size_t)row * Hkv + (w.h - Hq)) * D
+                                            : p.V_pages + ((size_t)row * Hkv + (w.h - Hq - Hkv)) * D;
         store8(dst + e0, x, 0);
         store8(dst + e1, x, 8);
     };
-    const int step = ROPE_WARPS * (int)gridDim.y;
-    for (int k = (int)blockIdx.y * ROPE_WARPS + warp; k < nt * groups; k += 2 * step) {     // two groups' loads in flight
-        const Row wa = row_of(k), wb = row_of(k + step);
-        float xa[16], xb[16];
-        load(wa, xa);
-        load(wb, xb);
+    while (true) {                                          // two groups' loads in flight
         finish(wa, xa);
         finish(wb, xb);
+        k += 2 * step;
+        if (k >= nt * groups) break;
+        wa = row_of(k); wb = row_of(k + step);
+        load(wa, xa);
+        load(wb, xb);
     }
     if (p.pos_cache != nullptr && blockIdx.y == 0)
         for (int x = tid; x < nt * Hkv; x += ROPE_THREADS) {
