@@ -258,8 +258,9 @@ seka_status seka_learn_projections(const seka_learn_shape* shape, const void* h,
  *  - One workspace of seka_paged_workspace_bytes(shape) bytes serves all calls, 256-byte aligned, first 256 bytes the status block.  A
  *    length, token offset or page number outside its range, found on the device, records SEKA_ERR_INVALID_ARG there; nothing outside
  *    the buffers is touched, the call's outputs are then undefined.  A launch on a workspace whose status is not SEKA_OK does nothing.
- *  - Calls that may run at the same time need a workspace each.  No two sequences may own the same page in a call that
- *    writes pages (seka_rope_append: the pages of the new rows; seka_evict_cache: any page of a sequence that is cut).
+ *  - Calls that may run at the same time, captured graphs among them, need a workspace each.  In a call that writes pages, no page that
+ *    is written may stand in the table twice (seka_rope_append: the pages of the new rows; seka_evict_cache: any page
+ *    of a sequence that is cut).  Sequences may share pages, a common prefix for instance, where they are only read.
  */
 typedef struct {
     int32_t batch;              /* number of sequences B (>= 0) */
@@ -352,7 +353,8 @@ seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_pages, void*
 
 /*
  * The first 256 bytes of a workspace are its status block (int32 words): word 0 the status, word 1 a code for the
- * wait that gave up.  Two more words are read by the fused forward and are there for tests of the failure path:
+ * wait that gave up.  Two more words are read by the fused forward, and by seka_paged_attention where sequences have
+ * more than 16 rows (new tokens x query heads of a KV head); they are there for tests of the failure path:
  * word 4 (non-zero n: CTA 0 leaves out the load of the n-th V/K pair of its first work item, so that a wait runs out)
  * and word 5 (limit of every device-side wait of that launch in microseconds; 0 means 2 s).  A launch on a workspace
  * whose status is not SEKA_OK does nothing.

@@ -277,6 +277,13 @@ def _fits(name: str, t: Optional[torch.Tensor], dtype, shape, device, packed: bo
         raise ValueError("%s must be contiguous" % name)
 
 
+def _scratch(t: torch.Tensor, device):
+    """The workspace of a paged call and its bytes."""
+    if t is None or t.dtype is not torch.uint8 or t.device != device or not t.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on %s (new_paged_workspace)" % device)
+    return t.data_ptr(), t.numel()
+
+
 def make_paged_shape(*, batch: int, max_new: int, total_new: int, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int,
                      n_pages: int, block_table: torch.Tensor, cache_lens: torch.Tensor, cu_new: Optional[torch.Tensor] = None,
                      dtype: torch.dtype = torch.bfloat16, softmax_scale: float = 0.0) -> SekaPagedShape:
@@ -346,8 +353,10 @@ def seka_rope_append(shape: SekaPagedShape, rope: Optional[SekaRope], Q, K, V, p
     st, dev, (T, Hq, d), Hkv = _on_device(shape), shape._device, shape._q, shape.n_kv_heads
     for name, x, H in (("Q", Q, Hq), ("K", K, Hkv), ("V", V, Hkv)):
         _fits(name, x, shape._dtype, (T, H, d), dev, packed=False)
-        if T > 0 and (x.stride(2) != 1 or (H > 1 and x.stride(1) != d)):
-            raise ValueError("%s: the heads of a token must be contiguous" % name)
+        if T > 0 and (x.stride(2) != 1 or (H > 1 and x.stride(1) != d) or (T > 1 and x.stride(0) < H * d)):
+            raise ValueError("%s: the heads of a token must be contiguous, its tokens apart" % name)
+    if rope is not None and rope._keepalive.device != dev:
+        raise ValueError("the turns are on %s, not on %s" % (rope._keepalive.device, dev))
     _fits("positions", positions, torch.int32, (T,), dev)
     _fits("Q_out", Q_out, torch.bfloat16, (T, Hq, d), dev)
     _fits("K_pages", K_pages, torch.bfloat16, shape._pages, dev)
@@ -356,7 +365,7 @@ def seka_rope_append(shape: SekaPagedShape, rope: Optional[SekaRope], Q, K, V, p
     strides = [x.stride(0) if T > 1 else 0 for x in (Q, K, V)]
     _check(load().seka_rope_append(ctypes.byref(shape), ctypes.byref(rope) if rope is not None else None, Q.data_ptr(), strides[0],
                                    K.data_ptr(), strides[1], V.data_ptr(), strides[2], _ptr(positions), _ptr(Q_out), _ptr(K_pages),
-                                   _ptr(V_pages), _ptr(pos_cache), _ptr(workspace), workspace.numel(), st), "seka_rope_append")
+                                   _ptr(V_pages), _ptr(pos_cache), *_scratch(workspace, dev), st), "seka_rope_append")
 
 
 def seka_paged_attention(shape: SekaPagedShape, Q, K_pages, V_pages, O, lse, workspace) -> None:
@@ -368,7 +377,7 @@ def seka_paged_attention(shape: SekaPagedShape, Q, K_pages, V_pages, O, lse, wor
     _fits("O", O, torch.bfloat16, shape._q, dev)
     _fits("lse", lse, torch.float32, shape._q[:2], dev)
     _check(load().seka_paged_attention(ctypes.byref(shape), _ptr(Q), _ptr(K_pages), _ptr(V_pages), _ptr(O), _ptr(lse),
-                                       _ptr(workspace), workspace.numel(), st), "seka_paged_attention")
+                                       *_scratch(workspace, dev), st), "seka_paged_attention")
 
 
 def seka_attention_mass(shape: SekaPagedShape, Q, K_pages, lse, mass_in, mass_out, workspace) -> None:
@@ -380,7 +389,7 @@ def seka_attention_mass(shape: SekaPagedShape, Q, K_pages, lse, mass_in, mass_ou
     _fits("mass_in", mass_in, torch.float32, shape._state, dev)
     _fits("mass_out", mass_out, torch.float32, shape._state, dev)
     _check(load().seka_attention_mass(ctypes.byref(shape), _ptr(Q), _ptr(K_pages), _ptr(lse), _ptr(mass_in), _ptr(mass_out),
-                                      _ptr(workspace), workspace.numel(), st), "seka_attention_mass")
+                                      *_scratch(workspace, dev), st), "seka_attention_mass")
 
 
 def seka_evict_cache(shape: SekaPagedShape, K_pages, V_pages, mass_in, mass_out, pos_in, pos_out, protect, next_pos, keep: int,
@@ -397,5 +406,5 @@ def seka_evict_cache(shape: SekaPagedShape, K_pages, V_pages, mass_in, mass_out,
     _fits("lens_out", lens_out, torch.int32, (B,), dev)
     _check(load().seka_evict_cache(ctypes.byref(shape), _ptr(K_pages), _ptr(V_pages), _ptr(mass_in), _ptr(mass_out), _ptr(pos_in),
                                    _ptr(pos_out), _ptr(protect), protect.shape[1] if protect is not None else 0, _ptr(next_pos),
-                                   int(keep), int(recent), _ptr(lens_out), _ptr(workspace), workspace.numel(), st),
+                                   int(keep), int(recent), _ptr(lens_out), *_scratch(workspace, dev), st),
            "seka_evict_cache")

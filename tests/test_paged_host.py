@@ -90,6 +90,12 @@ def test_bad_arguments(lib):
     assert binding.seka_launch_count() == 0
 
 
+def test_misaligned_state_is_refused(lib):
+    off = ctypes.c_void_p(ONE.value + 4)
+    assert evict(lib, shape(), m=off) == binding.SEKA_ERR_INVALID_ARG
+    assert evict(lib, shape(), p=off) == binding.SEKA_ERR_INVALID_ARG
+
+
 def test_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError):
         binding.make_paged_shape(batch=1, max_new=1, total_new=1, n_q_heads=2, n_kv_heads=1, head_dim=64, page_size=16, n_pages=4,
