@@ -351,10 +351,13 @@ def seka_rope_append(shape: SekaPagedShape, rope: Optional[SekaRope], Q, K, V, p
                      workspace) -> None:
     """Rotate the new queries and keys, cache keys and values.  Q, K, V may be slices of one projection (heads contiguous)."""
     st, dev, (T, Hq, d), Hkv = _on_device(shape), shape._device, shape._q, shape.n_kv_heads
+    strides = []
     for name, x, H in (("Q", Q, Hq), ("K", K, Hkv), ("V", V, Hkv)):
         _fits(name, x, shape._dtype, (T, H, d), dev, packed=False)
-        if T > 0 and (x.stride(2) != 1 or (H > 1 and x.stride(1) != d) or (T > 1 and x.stride(0) < H * d)):
+        token, head, one = x.stride()
+        if T > 0 and (one != 1 or (H > 1 and head != d) or (T > 1 and token < H * d)):
             raise ValueError("%s: the heads of a token must be contiguous, its tokens apart" % name)
+        strides.append(token if T > 1 else 0)
     if rope is not None and rope._keepalive.device != dev:
         raise ValueError("the turns are on %s, not on %s" % (rope._keepalive.device, dev))
     _fits("positions", positions, torch.int32, (T,), dev)
@@ -362,7 +365,6 @@ def seka_rope_append(shape: SekaPagedShape, rope: Optional[SekaRope], Q, K, V, p
     _fits("K_pages", K_pages, torch.bfloat16, shape._pages, dev)
     _fits("V_pages", V_pages, torch.bfloat16, shape._pages, dev)
     _fits("pos_cache", pos_cache, torch.int32, shape._state, dev)
-    strides = [x.stride(0) if T > 1 else 0 for x in (Q, K, V)]
     _check(load().seka_rope_append(ctypes.byref(shape), ctypes.byref(rope) if rope is not None else None, Q.data_ptr(), strides[0],
                                    K.data_ptr(), strides[1], V.data_ptr(), strides[2], _ptr(positions), _ptr(Q_out), _ptr(K_pages),
                                    _ptr(V_pages), _ptr(pos_cache), *_scratch(workspace, dev), st), "seka_rope_append")

@@ -288,19 +288,25 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
     }
 }
 
-// A block per (cut, 32 rows; 16 where a unit has no more): nothing to do where the share begins with a unit, or where an earlier cut of
-// the same unit does it.  A warp merges four rows at a time: the chain from the cut's record to the parts is four trips to memory long.
+// Blocks of 8 warps for every cut: nothing to do where the share begins with a unit, or where an earlier cut of the same unit does it.
+// The chain from the cut's record to the parts is four trips to memory long, so rows are merged four at a time.
+//   SPREAD false  units of a few parts: a block takes 32 rows, a warp four of them;
+//   SPREAD true   units of many parts (a long context on few heads): a block takes four rows and each warp an eighth of the
+//                 parts; the warps' sums are added in shared memory, in the order of the warps.
 constexpr int MERGE_WARPS = 8, MERGE_ROWS = 4;
-template <int D>
-__global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttnParams p, int unit_rows) {
+constexpr int merge_block_rows(bool spread) { return spread ? MERGE_ROWS : MERGE_WARPS * MERGE_ROWS; }
+template <int D, bool SPREAD>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttnParams p, int unit_rows, int live_rows) {
     constexpr int E = D / 32;
-    const int blocks = (unit_rows + MERGE_WARPS * MERGE_ROWS - 1) / (MERGE_WARPS * MERGE_ROWS), cut = (int)blockIdx.x / blocks;
-    const int r0 = (((int)blockIdx.x - cut * blocks) * MERGE_WARPS + (threadIdx.x >> 5)) * MERGE_ROWS, lane = threadIdx.x & 31;
+    __shared__ __align__(16) float sums[SPREAD ? MERGE_WARPS : 1][MERGE_ROWS][D];
+    const int blocks = (live_rows + merge_block_rows(SPREAD) - 1) / merge_block_rows(SPREAD), cut = (int)blockIdx.x / blocks;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r0 = ((int)blockIdx.x - cut * blocks) * merge_block_rows(SPREAD) + (SPREAD ? 0 : warp * MERGE_ROWS);
     pdl_wait();
     pdl_release();
     const int status0 = *p.v.status;
     const CutRecord c = p.cuts[cut];
-    if (status0 != 0 || r0 >= unit_rows || c.n == 0 || c.j == 0 || c.j > c.share) return;
+    if (status0 != 0 || r0 >= live_rows || c.n == 0 || c.j == 0 || c.j > c.share) return;
     const PagedSeq s = paged_seq(p.v, c.b);
     // parts: the last segment of share cut - 1, then the first ones of the shares on
     const int parts = 1 + (c.n - c.j + c.share - 1) / c.share;
@@ -309,13 +315,13 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
     bool real[MERGE_ROWS];
     bool any = false;
 #pragma unroll
-    for (int q = 0; q < MERGE_ROWS; ++q) {                  // row -> new token and query head
+    for (int q = 0; q < MERGE_ROWS; ++q) {              // row -> new token and query head
         const int r = r0 + q, tile = r >> 7, rt = r & 127, t_tile = rt / p.v.G, tok = c.p * p.geo.tp + tile * p.tile_tokens + t_tile;
         real[q] = t_tile < p.tile_tokens && tok < s.n;
         out[q] = (size_t)(s.q0 + tok) * p.v.Hq + (size_t)c.h * p.v.G + (rt - t_tile * p.v.G);
         any |= real[q];
     }
-    if (!any) return;
+    if (!any) return;                                       // (SPREAD: the same for the whole block)
     float M[MERGE_ROWS], l[MERGE_ROWS], acc[MERGE_ROWS][E];
 #pragma unroll
     for (int q = 0; q < MERGE_ROWS; ++q) {
@@ -337,13 +343,13 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
             for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
             const float keep = M[q] == -INFINITY ? 0.f : fast_exp2(M[q] - mx);
             f[q] = ml[q].x == -INFINITY ? 0.f : fast_exp2(ml[q].x - mx);
-            l[q] = fmaf(l[q], keep, ml[q].y * f[q]);        // per lane until the end
+            l[q] = fmaf(l[q], keep, ml[q].y * f[q]);    // per lane until the end
             M[q] = mx;
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[q][e] *= keep;
         }
 #pragma unroll 2
-        for (int i = 0; i < n; ++i) {
+        for (int i = SPREAD ? warp : 0; i < n; i += SPREAD ? MERGE_WARPS : 1) {
             const float* src = p.part_o + (slot(i0 + i) * unit_rows + r0) * D + lane * E;
             float x[MERGE_ROWS][E];
 #pragma unroll
@@ -359,11 +365,26 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
             }
         }
     }
+    if (SPREAD) {
+#pragma unroll
+        for (int q = 0; q < MERGE_ROWS; ++q)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sums[warp][q][lane * E + e] = acc[q][e];
+        __syncthreads();
+    }
 #pragma unroll
     for (int q = 0; q < MERGE_ROWS; ++q) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) l[q] += __shfl_xor_sync(0xffffffffu, l[q], o);
-        if (!real[q]) continue;
+        if (!real[q] || (SPREAD && warp != q)) continue;
+        if (SPREAD) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                acc[q][e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < MERGE_WARPS; ++w) acc[q][e] += sums[w][q][lane * E + e];
+            }
+        }
         const float inv = l[q] == 0.f ? 0.f : 1.f / l[q];
         uint32_t* dst = reinterpret_cast<uint32_t*>(p.O + out[q] * D + lane * E);
 #pragma unroll
@@ -433,8 +454,13 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
                        : launch_paged_tiles<64>(p, Q, K_pages, V_pages, shape->page_size, st);
     }
     if (stc != SEKA_OK || p.n_shares == 1) return stc;
-    const int rows = unit_rows(shape);
-    const unsigned grid = (unsigned)(p.n_shares * ((rows + MERGE_WARPS * MERGE_ROWS - 1) / (MERGE_WARPS * MERGE_ROWS)));
-    return D == 128 ? launch_kernel(true, paged_merge_kernel<128>, grid, MERGE_WARPS * 32, 0, st, p, rows)
-                    : launch_kernel(true, paged_merge_kernel<64>, grid, MERGE_WARPS * 32, 0, st, p, rows);
+    // Few rows and, from what the host knows, about four parts of a unit or more: spread over the warps.  One sequence of 1024 / 4096 /
+    // 65536 tokens on 8 KV heads, a new one each: 11.9 / 18.4 / 66.7 us with a warp per four rows, 10.5 / 12.5 / 52.7 so; tiles
+    // of rows have warps enough (128 rows over 8192 tokens, two sequences: 37.5 us, spread 51.7).
+    const bool spread = few && p.n_shares >= 4 * units * shape->n_kv_heads;
+    const int rows = unit_rows(shape), live = shape->max_new <= p.tile_tokens ? shape->max_new * G : rows;      // rows that can be real
+    const unsigned grid = (unsigned)(p.n_shares * ((live + merge_block_rows(spread) - 1) / merge_block_rows(spread)));
+    auto merge = D == 128 ? (spread ? paged_merge_kernel<128, true> : paged_merge_kernel<128, false>)
+                          : (spread ? paged_merge_kernel<64, true> : paged_merge_kernel<64, false>);
+    return launch_kernel(true, merge, grid, MERGE_WARPS * 32, 0, st, p, rows, live);
 }
