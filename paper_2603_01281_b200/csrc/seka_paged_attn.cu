@@ -427,7 +427,10 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     // of 64, 17 / 128 new tokens each: 184 / 186 us in units of two, 160 / 164 in units of one; 256 new tokens 228 / 249.
     p.geo.tp = few ? shape->max_new : shape->max_new <= p.tile_tokens ? p.tile_tokens : 2 * p.tile_tokens;
     p.geo.shift = few ? 6 : 7;
-    p.geo.min_share = 4;
+    // A share is worth a CTA of its own from two stages of 64 tokens on (one sequence of 128 / 777 / 2048 / 4096 tokens, 8 KV heads: 7.8 / 11.2 /
+    // 10.7 / 13.0 us; from four on 10.7 / 12.1 / 10.7 / 12.5; with one 25 at 4096), a share of tiles from four on (32 new tokens
+    // over 4096: 26.4 us, from two on 28.8).
+    p.geo.min_share = few ? 2 : 4;
     p.geo.max_units = (shape->max_new + p.geo.tp - 1) / p.geo.tp;
     // shares that can have a step, from what the host knows
     const long long units = few ? shape->batch : (long long)shape->total_new / p.geo.tp + shape->batch;
@@ -454,10 +457,10 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
                        : launch_paged_tiles<64>(p, Q, K_pages, V_pages, shape->page_size, st);
     }
     if (stc != SEKA_OK || p.n_shares == 1) return stc;
-    // Few rows and, from what the host knows, about four parts of a unit or more: spread over the warps.  One sequence of 1024 / 4096 /
-    // 65536 tokens on 8 KV heads, a new one each: 11.9 / 18.4 / 66.7 us with a warp per four rows, 10.5 / 12.5 / 52.7 so; tiles
+    // Few rows and, from what the host knows, about two parts of a unit or more: spread over the warps.  One sequence of 777 / 4096 /
+    // 65536 tokens on 8 KV heads, a new one: 12.9 / 18.4 / 66.7 us with a warp per four rows, 12.1 / 12.5 / 52.7 so; tiles
     // of rows have warps enough (128 rows over 8192 tokens, two sequences: 37.5 us, spread 51.7).
-    const bool spread = few && p.n_shares >= 4 * units * shape->n_kv_heads;
+    const bool spread = few && p.n_shares >= 2 * units * shape->n_kv_heads;
     const int rows = unit_rows(shape), live = shape->max_new <= p.tile_tokens ? shape->max_new * G : rows;      // rows that can be real
     const unsigned grid = (unsigned)(p.n_shares * ((live + merge_block_rows(spread) - 1) / merge_block_rows(spread)));
     auto merge = D == 128 ? (spread ? paged_merge_kernel<128, true> : paged_merge_kernel<128, false>)
