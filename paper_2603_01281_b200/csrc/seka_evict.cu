@@ -12,6 +12,8 @@
 //                         kept ones behind, every warp on consecutive rows so that ranks come from ballots.  Four rows a lane
 //                         at a time: with many pairs the passes are bound by instructions, not by memory.
 //   evict_move_kernel     copies K, V, weight and position of the kept rows behind into the freed rows.
+// 64 contexts of 1024 to 4096 rows, 8 KV heads of 128, cut to 2048: 80 us = 30 (selection) + 50 (233 MB in pieces of 256 bytes, 4.1 TB/s);
+// one of 65536 cut to 16384: 56 us = 27 (a chain of passes and cluster barriers) + 24.
 // What is kept below `keep` does not move: a cache that is cut often, by a little each time, moves only that little.  Sources lie at or
 // behind `keep`, destinations below it, so the copies need no order.
 #include <math.h>
@@ -492,12 +494,14 @@ extern "C" seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_p
     const unsigned pairs = (unsigned)shape->batch * (unsigned)shape->n_kv_heads;
     int n_sm = 0;
     if (!device_info(&n_sm)) return SEKA_ERR_CUDA;
-    // CTAs of a pair: more while they still find SMs and have 2048 rows each (a cache may be filled to its last page)
+    // CTAs of a pair: more while they still find SMs and have 2048 rows each (a cache may be filled to its last page).  One context of 65536
+    // rows: 56 us, 235 with one CTA a pair; 8 of 8192: 51 and 56.
     p.cluster = 1;
     while (p.cluster < EV_MAX_CLUSTER && 2LL * p.cluster * pairs <= 2LL * n_sm && p.v.cap > 4 * 1024 * p.cluster) p.cluster *= 2;
     const int lanes = p.cluster * EV_WARPS * 128;
     const long long rows = ((long long)p.v.cap + lanes - 1) / lanes * (EV_WARPS * 128);     // most rows of a CTA
-    p.cached = rows <= EV_MAX_CACHED ? (int)rows : 0;                                       // longer: ranks are formed again in every pass
+    // longer: ranks are formed again in every pass (one context of 65536 that way: 78 us, 56 cached; 64 of 1024 to 4096: 92 and 80)
+    p.cached = rows <= EV_MAX_CACHED ? (int)rows : 0;
     const size_t bytes = sizeof(EvSmem) + (size_t)p.cached * 5;
     if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return SEKA_ERR_CUDA;
     stc = launch_cluster(true, (unsigned)p.cluster, evict_select_kernel, dim3(pairs * (unsigned)p.cluster), EV_THREADS, bytes, st, p);
@@ -505,8 +509,10 @@ extern "C" seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_p
     const int D = shape->head_dim;
     const long long most = p.v.cap - keep < keep ? p.v.cap - keep : keep;          // rows of a pair that can move
     const long long fill = (16LL * n_sm + pairs - 1) / pairs;
+    // rows of a warp: eight while that leaves fewer than eight warps per SM, up to 32 (64 contexts 80 us, 86 with eight always; one of
+    // 1500 15.6, 17.6 with 32 always)
     p.move_rows = 32;
-    while (p.move_rows > 8 && (long long)pairs * most < 8LL * n_sm * p.move_rows) p.move_rows /= 2;      // (fewer than eight warps per SM)
+    while (p.move_rows > 8 && (long long)pairs * most < 8LL * n_sm * p.move_rows) p.move_rows /= 2;
     long long blocks = most > 0 ? (most + MV_WARPS * p.move_rows - 1) / (MV_WARPS * p.move_rows) : 1;
     if (blocks > fill) blocks = fill;
     p.move_blocks = (int)blocks;

@@ -4,9 +4,12 @@
 // The score tile is formed with the KEYS as its rows, so that the sum over queries runs along a thread's own row: no reduction
 // between threads, no atomics, a fixed order.  K is read once, V not at all.
 //   mass_few_kernel       up to 16 query rows: bound by HBM.  A producer warp streams 64-token stages of K (TMA, a box per piece of a
-//                         page); four consumer warps take 16 tokens each, mma.sync m16n8k16 with K as A and the queries as B.
+//                         page); four consumer warps take 16 tokens each, mma.sync m16n8k16 with K as A and the queries as B.  64 contexts of
+//                         1024 to 4096 tokens, 32/8 heads of 128 (343 MB): 64 us, 5.3 TB/s; the floor is 53.
 //   mass_tile_kernel      more rows, on tcgen05: 2 x 128 cached tokens stay in shared memory, tiles of 128 query rows (new token r / G,
 //                         head r % G) pass by.  Bound by the exponentials (one per score, against 2 d flops).
+//                         2 x 1024 tokens over 6000 to 8192, 32/8 heads of 128: 165 us, of which 105 are exponentials at the rate of the
+//                         special-function unit (57 % busy; a quarter of them run on the multiply-add pipe instead).
 //   mass_merge_kernel     adds the parts of a unit that a share boundary cut.
 #include <math.h>
 

@@ -6,7 +6,8 @@
 //                         the scores of all rows with mma.sync m16n8k16 (16 rows are too few for a tcgen05 tile), keep
 //                         a private online softmax and P V in registers.  The CTA walks its equal share of all stages, unit after
 //                         unit, without the ring running dry between them.
-//   paged_merge_kernel    merges the parts of a unit that a share boundary cut, a warp per row.
+//                         64 contexts of 1024 to 4096 tokens, 32/8 heads of 128 (666 MB): 112 us, 5.9 TB/s; the floor is 103.
+//   paged_merge_kernel    merges the parts of a unit that a share boundary cut: 4 us of a single sequence's 11, four trips to memory.
 // Weights are rounded to bf16 for P V (half a step, 2^-8 of each); scores, sums and outputs stay in fp32 until the store.
 #include <math.h>
 
@@ -42,7 +43,8 @@ __device__ __forceinline__ bool consumer_sync_or(bool x) {
     return r != 0;
 }
 
-// HALF: at most 8 rows, so rows 8..15 of every MMA are padding and their softmax is skipped.
+// HALF: at most 8 rows, so rows 8..15 of every MMA are padding and their softmax is skipped (8 contexts of 1024 to 4096 tokens, a new token
+// each: 23.1 us, 24.9 without; with 64 contexts HBM hides it, 115 and 116).
 template <int D, bool HALF>
 __global__ void __launch_bounds__(FEW_THREADS, FewSmem<D>::CTAS_PER_SM)
 paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ PagedAttnParams p) {
