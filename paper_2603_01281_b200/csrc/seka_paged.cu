@@ -20,7 +20,10 @@ seka_status validate_paged(const seka_paged_shape* s) {
     if (s->n_q_heads / s->n_kv_heads > 128 || s->n_q_heads > 32767 || s->batch > 65535) return SEKA_ERR_UNSUPPORTED;
     // rows of a sequence and of the pool, and tokens, are counted in 31 bits (bytes and elements in 64)
     if ((long long)s->max_pages * s->page_size > 0x7fff0000LL || (long long)s->n_pages * s->page_size > 0x7fff0000LL ||
-        (long long)s->batch * s->n_kv_heads > 0x7fffffffLL) return SEKA_ERR_UNSUPPORTED;
+        s->max_new > 0x7fff0000 || s->total_new > 0x7fff0000) return SEKA_ERR_UNSUPPORTED;
+    // state rows, and with them the workspace, are counted in 64 bits
+    const long long pairs = (long long)s->batch * s->n_kv_heads, cap = (long long)s->max_pages * s->page_size;
+    if (pairs > 0x7fffffffLL || pairs * cap > 1LL << 40) return SEKA_ERR_UNSUPPORTED;
     return SEKA_OK;
 }
 

@@ -410,7 +410,7 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     using namespace seka;
     seka_status stc = validate_paged(shape);
     if (stc != SEKA_OK) return stc;
-    if (shape->batch == 0 || shape->total_new == 0) return SEKA_OK;
+    if (shape->batch == 0 || shape->total_new == 0 || shape->max_new == 0) return SEKA_OK;      // no sequence owns a token
     if (!Q || !O || !K_pages || !V_pages) return SEKA_ERR_INVALID_ARG;
     if (((uintptr_t)Q | (uintptr_t)K_pages | (uintptr_t)V_pages | (uintptr_t)O) & 15) return SEKA_ERR_INVALID_ARG;
     stc = check_paged_call(shape, workspace, workspace_bytes);

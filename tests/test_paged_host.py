@@ -229,3 +229,16 @@ def test_division_among_ctas_on_the_host(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-I", build.CSRC, "-I", cuda, str(src), "-o", str(exe)], check=True)
     out = subprocess.run([str(exe)], capture_output=True, text=True)
     assert out.returncode == 0, out.stdout
+
+
+def test_no_sequence_has_new_tokens(lib):
+    # a padded packed step in which every sequence is idle: tokens that nobody owns, nothing to attend to
+    assert attend(lib, shape(max_new=0)) == binding.SEKA_OK
+
+
+def test_counts_beyond_their_bits_are_refused(lib):
+    for bad in (dict(max_new=(1 << 31) - 1), dict(total_new=(1 << 31) - 1), dict(batch=60000, n_kv_heads=30000, n_q_heads=30000, max_pages=1 << 24, n_pages=1 << 20)):
+        s = shape(**bad)
+        assert lib.seka_paged_workspace_bytes(ctypes.byref(s)) == 0
+        for call in (append, attend, mass, evict):
+            assert call(lib, s) == binding.SEKA_ERR_UNSUPPORTED, (bad, call)
