@@ -9,10 +9,10 @@
 //   NEIGHBOURS  interleaved pairs: 16 consecutive elements, any r (also what is not rotated at all);
 //   HALVES      pairs r/2 apart with r a multiple of 16: eight elements and their eight partners, both on 16-byte boundaries;
 //   STAGED      pairs r/2 apart at no alignment: the warp's rows go through shared memory, a lane per pair there (16384 tokens of
-//               32/8 heads of 128: 103 us, 88 as HALVES).
-// The loads of the first rows are issued before the token's sequence, page and angles are known (100 -> 88 us). 16384 tokens of 32/8 heads of
-// 128 in bf16 (403 MB): 88 us, 4.6 TB/s; some 16000 tokens of 16/16 heads of 64 in fp32 (313 MB): 55 us, 5.7 TB/s; 64 tokens:
-// 6.3 us on the device, less than the call's work on the host.
+//               32/8 heads of 128: 103 us where HALVES took 88).
+// The loads of the first rows are issued before the token's sequence, page and angles are known (100 -> 88 us); three groups of rows are in flight
+// as bf16, two as fp32.  16384 tokens of 32/8 heads of 128 in bf16 (403 MB): 82 us, 4.9 TB/s; some 16000 tokens of 16/16 heads of 64 in fp32
+// (313 MB): 56 us, 5.6 TB/s; 64 tokens: 6.3 us on the device, less than the call's work on the host.
 #include "seka_kernels.h"
 #include "seka_paged.cuh"
 
@@ -51,13 +51,28 @@ template <typename T> __device__ __forceinline__ void load8(const T* p, float (&
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[16], int at) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[at], x[at + 1]), pack_bf16(x[at + 2], x[at + 3]), pack_bf16(x[at + 4], x[at + 5]), pack_bf16(x[at + 6], x[at + 7]));
 }
+// a lane's sixteen elements on their way: bf16 as it lies in memory, half the registers
+template <typename T> struct Flying;
+template <> struct Flying<float> {
+    float v[16];
+    __device__ __forceinline__ void fetch(const float* a, const float* b) { load8(a, v, 0); load8(b, v, 8); }
+};
+template <> struct Flying<__nv_bfloat16> {
+    uint4 v[2];
+    __device__ __forceinline__ void fetch(const __nv_bfloat16* a, const __nv_bfloat16* b) {
+        v[0] = *reinterpret_cast<const uint4*>(a); v[1] = *reinterpret_cast<const uint4*>(b);
+    }
+    __device__ __forceinline__ void unpack(float (&x)[16]) const {
+        load8(reinterpret_cast<const __nv_bfloat16*>(&v[0]), x, 0); load8(reinterpret_cast<const __nv_bfloat16*>(&v[1]), x, 8);
+    }
+};
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void put(float& d, float x) { d = x; }
 __device__ __forceinline__ void put(__nv_bfloat16& d, float x) { d = __float2bfloat16(x); }
 
 enum RopeMode { NEIGHBOURS, HALVES, STAGED };
-constexpr int ROPE_WARPS = ROPE_THREADS / 32, ROPE_TOKENS = 4;
+constexpr int ROPE_WARPS = ROPE_THREADS / 32, ROPE_TOKENS = 8;        // most tokens of a block
 
 template <typename T, int D, RopeMode MODE>
 __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopeParams p, int tokens) {
@@ -87,28 +102,30 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopePar
         w.have = w.i < nt && w.h < n_rows;
         return w;
     };
-    auto load = [&](const Row& w, float (&x)[16]) {
+    auto load = [&](const Row& w, Flying<T>& x) {
         if (!w.have) return;
         const size_t t = (size_t)(t0 + w.i);
         const T* src = w.h < Hq ? static_cast<const T*>(p.Q) + t * p.q_stride + (size_t)w.h * D
                      : w.h < Hq + Hkv ? static_cast<const T*>(p.K) + t * p.k_stride + (size_t)(w.h - Hq) * D
                                       : static_cast<const T*>(p.V) + t * p.v_stride + (size_t)(w.h - Hq - Hkv) * D;
-        load8(src + e0, x, 0);
-        load8(src + e1, x, 8);
+        x.fetch(src + e0, src + e1);
     };
     // the first rows are on their way while the tokens' sequences, pages and angles are found
     const int step = ROPE_WARPS * (int)gridDim.y;
     int k = (int)blockIdx.y * ROPE_WARPS + warp;
-    Row wa = row_of(k), wb = row_of(k + step);
-    float xa[16], xb[16];
-    load(wa, xa);
-    load(wb, xb);
+    constexpr int FLIGHT = sizeof(T) == 2 ? 3 : 2;          // groups of rows in flight
+    Row w[FLIGHT];
+    Flying<T> v[FLIGHT];
+#pragma unroll
+    for (int f = 0; f < FLIGHT; ++f) { w[f] = row_of(k + f * step); load(w[f], v[f]); }
     // the sequences that own the tokens
     for (int b = tid; b < p.v.B; b += ROPE_THREADS) {
         const int q0 = p.v.cu ? p.v.cu[b] : b * p.v.max_new, q1 = p.v.cu ? p.v.cu[b + 1] : q0 + p.v.max_new;
-        if (q0 >= t0 + nt || q1 <= t0) continue;
+        const bool here = q0 < t0 + nt && q1 > t0;
+        if (!here && (blockIdx.x != 0 || blockIdx.y != 0)) continue;                    // (the first block looks at every sequence)
         const PagedSeq s = check_seq(p.v, q0, q1, p.v.lens[b]);
-        if (!s.valid) { report_invalid(p.v.status, kWhereSeq); continue; }
+        if (!s.valid) report_invalid(p.v.status, kWhereSeq);
+        if (!s.valid || !here) continue;
         for (int i = max(0, q0 - t0); i < min(nt, q1 - t0); ++i) {
             const int j = s.L - s.n + (t0 + i - q0);
             tok[i][0] = b; tok[i][1] = j;
@@ -178,14 +195,21 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopePar
         store8(dst + e0, x, 0);
         store8(dst + e1, x, 8);
     };
-    while (true) {                                          // two groups' loads in flight
-        finish(wa, xa);
-        finish(wb, xb);
-        k += 2 * step;
+    while (true) {
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            if constexpr (sizeof(T) == 2) {
+                float x[16];
+                v[f].unpack(x);
+                finish(w[f], x);
+            } else {
+                finish(w[f], v[f].v);
+            }
+        }
+        k += FLIGHT * step;
         if (k >= nt * groups) break;
-        wa = row_of(k); wb = row_of(k + step);
-        load(wa, xa);
-        load(wb, xb);
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) { w[f] = row_of(k + f * step); load(w[f], v[f]); }
     }
     if (p.pos_cache != nullptr && blockIdx.y == 0)
         for (int x = tid; x < nt * Hkv; x += ROPE_THREADS) {
@@ -200,9 +224,11 @@ seka_status launch_rope(const RopeParams& p, cudaStream_t st) {
     int n_sm = 0;
     if (!device_info(&n_sm)) return SEKA_ERR_CUDA;
     const int groups = (p.v.Hq + 2 * p.v.Hkv + 512 / D - 1) / (512 / D);        // of a token's rows: a warp's worth each
-    // four tokens a block where that still gives every SM a few blocks (16384 tokens: 88 us, 124 with one a block); else one, and blocks
-    // share a token as far as it has rows (a trip to memory less in the chain of a block; within the noise of a call at 64 tokens)
-    const int tokens = p.v.T >= ROPE_TOKENS * 4 * n_sm ? ROPE_TOKENS : 1;
+    // four tokens a block, in bf16 eight, where that still gives every SM four blocks (16384 tokens of 32/8 heads in bf16: 82 us, 83 with four,
+    // 124 with one a block; 3000: 18 with four, 27 with one; some 16000 in fp32 56, 57 with eight); else one, and blocks share a token as far
+    // as it has rows
+    const long long each = 4LL * n_sm;
+    const int tokens = sizeof(T) == 2 && p.v.T >= 8 * each ? 8 : p.v.T >= 4 * each ? 4 : 1;
     int split = 1;
     while (tokens == 1 && split * ROPE_WARPS < groups && (long long)p.v.T * split < 2LL * n_sm) ++split;
     const dim3 grid((unsigned)((p.v.T + tokens - 1) / tokens), (unsigned)split);

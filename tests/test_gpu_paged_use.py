@@ -316,3 +316,42 @@ def test_refused_tensors():
     with pytest.raises(ValueError):
         binding.seka_attention_mass(c.shape, c.Q, c.K, s.lse, s.mass[:, :, :-1], s.mass, c.ws)
     assert c.status() == binding.SEKA_OK and same(s.everything(), before)
+
+
+def test_a_step_without_new_tokens():
+    # a padded packed step in which every sequence is idle: tokens are rotated, nothing is stored, attended to or weighed
+    c = R.Cache([100, 40], [0, 0], 4, 2, 64, 16, seed=35)
+    shape = binding.make_paged_shape(batch=2, max_new=0, total_new=3, n_q_heads=4, n_kv_heads=2, head_dim=64, page_size=16, n_pages=c.n_pages,
+                                     block_table=c.table_d, cache_lens=c.lens_d, cu_new=c.cu_d)
+    ws = binding.new_paged_workspace(shape)
+    qkv = torch.randn((3, 8, 64), generator=c.g).bfloat16().cuda()
+    Q, O, lse = torch.zeros_like(qkv[:, :4]), torch.full((3, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda"), torch.full((3, 4), 3.0, device="cuda")
+    Q, K0, V0 = Q.contiguous(), c.K.clone(), c.V.clone()
+    pos = torch.tensor([7, 8, 9], dtype=torch.int32, device="cuda")
+    turns = binding.seka_rope_turns(64).cuda()
+    binding.seka_rope_append(shape, binding.make_rope(turns), qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], pos, Q, c.K, c.V, None, ws)
+    binding.seka_paged_attention(shape, Q, c.K, c.V, O, lse, ws)
+    m0 = torch.rand((2, 2, c.cap), generator=c.g).cuda()
+    m = torch.full_like(m0, -7.0)
+    binding.seka_attention_mass(shape, Q, c.K, lse, m0, m, ws)
+    assert binding.seka_poll_status(ws) == binding.SEKA_OK
+    want, size = R.rotate(qkv[:, :4], pos, turns, "half")
+    assert ((Q.double() - want).abs() <= HALF * want.abs() + 2.0 ** -20 * size).all()
+    assert same([c.K, c.V], [K0, V0]) and (O == 3.0).all() and (lse == 3.0).all()
+    inside = (torch.arange(c.cap, device="cuda")[None] < c.lens_d[:, None])[:, None].expand_as(m)
+    assert torch.equal(m[inside], m0[inside]) and (m[~inside] == -7.0).all()
+
+
+def test_every_sequence_is_looked_at():
+    # offsets and lengths out of range that own none of the call's tokens are reported too
+    for spoil in (lambda c: c.lens_d[2:].fill_(c.cap + 1), lambda c: c.lens_d[2:].fill_(-5), lambda c: c.cu_d[2:].copy_(torch.tensor([33, 1000]))):
+        c = R.Cache([100, 40, 30], [30, 3, 0], 4, 2, 64, 16, seed=36)
+        spoil(c)
+        x = torch.zeros((c.T, 8, 64), dtype=torch.bfloat16, device="cuda")
+        calls = [lambda: binding.seka_rope_append(c.shape, None, x[:, :4], x[:, 4:6], x[:, 6:], None, torch.empty_like(c.Q), c.K, c.V, None, c.ws),
+                 lambda: binding.seka_paged_attention(c.shape, c.Q, c.K, c.V, torch.empty_like(c.Q), None, c.ws),
+                 lambda: binding.seka_attention_mass(c.shape, c.Q, c.K, torch.zeros((c.T, 4), device="cuda"), None, torch.zeros((3, 2, c.cap), device="cuda"), c.ws)]
+        for call in calls:
+            call()
+            assert c.status() == binding.SEKA_ERR_INVALID_ARG
+            binding.seka_reset_status(c.ws)
