@@ -291,19 +291,20 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
 }
 
 // Blocks of 8 warps for every cut: nothing to do where the share begins with a unit, or where an earlier cut of the same unit does it.
-// The chain from the cut's record to the parts is four trips to memory long, so rows are merged four at a time.
+// The chain from the cut's record to the parts is four trips to memory long, so rows are merged a few at a time.
 //   SPREAD false  units of a few parts: a block takes 32 rows, a warp four of them;
-//   SPREAD true   units of many parts (a long context on few heads): a block takes four rows and each warp an eighth of the
-//                 parts; the warps' sums are added in shared memory, in the order of the warps.
-constexpr int MERGE_WARPS = 8, MERGE_ROWS = 4;
-constexpr int merge_block_rows(bool spread) { return spread ? MERGE_ROWS : MERGE_WARPS * MERGE_ROWS; }
+//   SPREAD true   units of many parts (a long context on few heads): a block takes two rows and each warp an eighth of the
+//                 parts; the warps' sums are added in shared memory, in the order of the warps (four rows: 1 us more).
+constexpr int MERGE_WARPS = 8;
+constexpr int merge_rows(bool spread) { return spread ? 2 : 4; }                 // of a warp at a time
+constexpr int merge_block_rows(bool spread) { return merge_rows(spread) * (spread ? 1 : MERGE_WARPS); }
 template <int D, bool SPREAD>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttnParams p, int unit_rows, int live_rows) {
-    constexpr int E = D / 32;
-    __shared__ __align__(16) float sums[SPREAD ? MERGE_WARPS : 1][MERGE_ROWS][D];
+    constexpr int E = D / 32, ROWS = merge_rows(SPREAD);
+    __shared__ __align__(16) float sums[SPREAD ? MERGE_WARPS : 1][ROWS][D];
     const int blocks = (live_rows + merge_block_rows(SPREAD) - 1) / merge_block_rows(SPREAD), cut = (int)blockIdx.x / blocks;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int r0 = ((int)blockIdx.x - cut * blocks) * merge_block_rows(SPREAD) + (SPREAD ? 0 : warp * MERGE_ROWS);
+    const int r0 = ((int)blockIdx.x - cut * blocks) * merge_block_rows(SPREAD) + (SPREAD ? 0 : warp * ROWS);
     pdl_wait();
     pdl_release();
     const int status0 = *p.v.status;
@@ -313,33 +314,33 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
     // parts: the last segment of share cut - 1, then the first ones of the shares on
     const int parts = 1 + (c.n - c.j + c.share - 1) / c.share;
     auto slot = [&](int i) -> size_t { return i == 0 ? (size_t)(cut - 1) * 2 + (c.j < c.share ? 1 : 0) : (size_t)(cut - 1 + i) * 2; };
-    size_t out[MERGE_ROWS];
-    bool real[MERGE_ROWS];
+    size_t out[ROWS];
+    bool real[ROWS];
     bool any = false;
 #pragma unroll
-    for (int q = 0; q < MERGE_ROWS; ++q) {              // row -> new token and query head
+    for (int q = 0; q < ROWS; ++q) {              // row -> new token and query head
         const int r = r0 + q, tile = r >> 7, rt = r & 127, t_tile = rt / p.v.G, tok = c.p * p.geo.tp + tile * p.tile_tokens + t_tile;
         real[q] = t_tile < p.tile_tokens && tok < s.n;
         out[q] = (size_t)(s.q0 + tok) * p.v.Hq + (size_t)c.h * p.v.G + (rt - t_tile * p.v.G);
         any |= real[q];
     }
     if (!any) return;                                       // (SPREAD: the same for the whole block)
-    float M[MERGE_ROWS], l[MERGE_ROWS], acc[MERGE_ROWS][E];
+    float M[ROWS], l[ROWS], acc[ROWS][E];
 #pragma unroll
-    for (int q = 0; q < MERGE_ROWS; ++q) {
+    for (int q = 0; q < ROWS; ++q) {
         M[q] = -INFINITY; l[q] = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[q][e] = 0.f;
     }
     for (int i0 = 0; i0 < parts; i0 += 32) {
         const int n = min(32, parts - i0);
-        float2 ml[MERGE_ROWS];
-        float f[MERGE_ROWS];
+        float2 ml[ROWS];
+        float f[ROWS];
 #pragma unroll
-        for (int q = 0; q < MERGE_ROWS; ++q)
+        for (int q = 0; q < ROWS; ++q)
             ml[q] = lane < n ? *reinterpret_cast<const float2*>(p.part_ml + (slot(i0 + lane) * unit_rows + r0 + q) * 2) : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int q = 0; q < MERGE_ROWS; ++q) {
+        for (int q = 0; q < ROWS; ++q) {
             float mx = fmaxf(M[q], ml[q].x);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -353,14 +354,14 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
 #pragma unroll 2
         for (int i = SPREAD ? warp : 0; i < n; i += SPREAD ? MERGE_WARPS : 1) {
             const float* src = p.part_o + (slot(i0 + i) * unit_rows + r0) * D + lane * E;
-            float x[MERGE_ROWS][E];
+            float x[ROWS][E];
 #pragma unroll
-            for (int q = 0; q < MERGE_ROWS; ++q) {
+            for (int q = 0; q < ROWS; ++q) {
                 if (E == 4) *reinterpret_cast<float4*>(x[q]) = *reinterpret_cast<const float4*>(src + q * D);
                 else *reinterpret_cast<float2*>(x[q]) = *reinterpret_cast<const float2*>(src + q * D);
             }
 #pragma unroll
-            for (int q = 0; q < MERGE_ROWS; ++q) {
+            for (int q = 0; q < ROWS; ++q) {
                 const float fi = __shfl_sync(0xffffffffu, f[q], i);
 #pragma unroll
                 for (int e = 0; e < E; ++e) acc[q][e] = fmaf(x[q][e], fi, acc[q][e]);
@@ -369,13 +370,13 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) paged_merge_kernel(const __g
     }
     if (SPREAD) {
 #pragma unroll
-        for (int q = 0; q < MERGE_ROWS; ++q)
+        for (int q = 0; q < ROWS; ++q)
 #pragma unroll
             for (int e = 0; e < E; ++e) sums[warp][q][lane * E + e] = acc[q][e];
         __syncthreads();
     }
 #pragma unroll
-    for (int q = 0; q < MERGE_ROWS; ++q) {
+    for (int q = 0; q < ROWS; ++q) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) l[q] += __shfl_xor_sync(0xffffffffu, l[q], o);
         if (!real[q] || (SPREAD && warp != q)) continue;
