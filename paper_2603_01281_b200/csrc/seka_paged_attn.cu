@@ -7,7 +7,7 @@
 //                         a private online softmax and P V in registers.  The CTA walks its equal share of all stages, unit after
 //                         unit, without the ring running dry between them.
 //                         64 contexts of 1024 to 4096 tokens, 32/8 heads of 128 (666 MB): 112 us, 5.9 TB/s; the floor is 103.
-//   paged_merge_kernel    merges the parts of a unit that a share boundary cut: 4 us of a single sequence's 11, four trips to memory.
+//   paged_merge_kernel    merges the parts of a unit that a share boundary cut: some 3 us of a single sequence's 11, four trips to memory.
 // Weights are rounded to bf16 for P V (half a step, 2^-8 of each); scores, sums and outputs stay in fp32 until the store.
 #include <math.h>
 
@@ -430,9 +430,9 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     // of 64, 17 / 128 new tokens each: 184 / 186 us in units of two, 160 / 164 in units of one; 256 new tokens 228 / 249.
     p.geo.tp = few ? shape->max_new : shape->max_new <= p.tile_tokens ? p.tile_tokens : 2 * p.tile_tokens;
     p.geo.shift = few ? 6 : 7;
-    // A share is worth a CTA of its own from two stages of 64 tokens on (one sequence of 128 / 777 / 2048 / 4096 tokens, 8 KV heads: 7.8 / 11.2 /
-    // 10.7 / 13.0 us; from four on 10.7 / 12.1 / 10.7 / 12.5; with one 25 at 4096), a share of tiles from four on (32 new tokens
-    // over 4096: 26.4 us, from two on 28.8).
+    // A share is worth a CTA of its own from two stages of 64 tokens on (one sequence of 128 / 777 / 2048 / 4096 tokens, 8 KV heads, in a graph: 7.8 /
+    // 10.5 / 9.8 / 11.9 us; from four on 10.7 / 11.7 / 10.2 / 11.8), a share of tiles from four on (32 new tokens over 4096: 20.7 us, from two
+    // on 22.5; over 1024 17.2 and 16.3).
     p.geo.min_share = few ? 2 : 4;
     p.geo.max_units = (shape->max_new + p.geo.tp - 1) / p.geo.tp;
     // shares that can have a step, from what the host knows
@@ -461,7 +461,7 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     }
     if (stc != SEKA_OK || p.n_shares == 1) return stc;
     // Few rows and, from what the host knows, about two parts of a unit or more: spread over the warps.  One sequence of 777 / 4096 /
-    // 65536 tokens on 8 KV heads, a new one: 12.9 / 18.4 / 66.7 us with a warp per four rows, 12.1 / 12.5 / 52.7 so; tiles
+    // 65536 tokens on 8 KV heads, a new one: 12.9 / 20.2 / 62.1 us with a warp per four rows, 10.5 / 11.9 / 52.3 so; tiles
     // of rows have warps enough (128 rows over 8192 tokens, two sequences: 37.5 us, spread 51.7).
     const bool spread = few && p.n_shares >= 2 * units * shape->n_kv_heads;
     const int rows = unit_rows(shape), live = shape->max_new <= p.tile_tokens ? shape->max_new * G : rows;      // rows that can be real
