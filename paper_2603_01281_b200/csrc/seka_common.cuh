@@ -486,13 +486,14 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return y;
 }
 
-// Two powers of two on the multiply-add pipe, beside the special-function unit (16 a clock and SM).  2^x = 2^n 2^f with n = rint(x) (the low
-// bits of x + 1.5 2^23), |f| <= 1/2; 2^f by the polynomial of degree 5 with the least largest relative error there (Remez exchange:
-// 7.5e-8, 2.1e-7 with the rounding of its steps); n goes into the exponent.  x <= 126; below -126 the result is 2^-126; NaN stays.
+// Two powers of two on the multiply-add pipe, beside the special-function unit (16 a clock and SM).  2^x = 2^n 2^f with n = rint(x), |f| <= 1/2;
+// 2^f by the polynomial of degree 5 with the least largest relative error there (Remez exchange: 7.5e-8, 2.1e-7 with the rounding of
+// its steps).  The low bits of x + 1.5 2^23 + 127 are n + 127, the exponent of 2^n.  That is a factor, not an addition to the exponent: NaN
+// stays NaN then (an integer sum would turn it into a finite number), and x <= -126.5, -infinity too, gives 0.  x <= 127.
 __device__ __forceinline__ float2 exp2_poly2(float2 x) {
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(x.x));      // -126
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(x.y));
-    const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f)), r = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.x));      // -127
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.y));
+    const float2 t = __fadd2_rn(x, make_float2(12583039.f, 12583039.f)), r = __fadd2_rn(t, make_float2(-12583039.f, -12583039.f));
     const float2 f = __ffma2_rn(r, make_float2(-1.f, -1.f), x);
     auto c = [](float v) { return make_float2(v, v); };
     float2 p = __ffma2_rn(c(0.0013276472454890609f), f, c(0.009675540961325169f));
@@ -500,7 +501,7 @@ __device__ __forceinline__ float2 exp2_poly2(float2 x) {
     p = __ffma2_rn(p, f, c(0.24022120237350464f));
     p = __ffma2_rn(p, f, c(0.6931469440460205f));
     p = __ffma2_rn(p, f, c(1.0000001192092896f));
-    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+    return __fmul2_rn(p, make_float2(__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)));
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
