@@ -257,7 +257,8 @@ seka_status seka_learn_projections(const seka_learn_shape* shape, const void* h,
  *    behind cache_lens[b] are never used and never written.  These arrays are 16-byte aligned.
  *  - One workspace of seka_paged_workspace_bytes(shape) bytes serves all calls, 256-byte aligned, first 256 bytes the status block.  A
  *    length, token offset or page number outside its range, found on the device, records SEKA_ERR_INVALID_ARG there; nothing outside
- *    the buffers is touched, the call's outputs are then undefined.  A launch on a workspace whose status is not SEKA_OK does nothing.
+ *    the buffers is touched, the call's outputs are then undefined.  Work of more than 2^30 steps (128 cached tokens under 256 rows, or 256
+ *    under 128) of an SM, more than twenty minutes, records SEKA_ERR_UNSUPPORTED.  A launch on a workspace whose status is not SEKA_OK does nothing.
  *  - Calls that may run at the same time, captured graphs among them, need a workspace each.  In a call that writes pages, no page that
  *    is written may stand in the table twice (seka_rope_append: the pages of the new rows; seka_evict_cache: any page
  *    of a sequence that is cut).  Sequences may share pages, a common prefix for instance, where they are only read.

@@ -540,6 +540,7 @@ extern "C" seka_status seka_attention_mass(const seka_paged_shape* shape, const 
     p.scale_log2 = scale * kLog2e;
     p.key = KeyGeo{6, 4, 1};
     p.rowg = RowGeo{128 / G, 8, 2, (p.v.cap + 255) / 256};
+    if (p.rowg.max_units <= 8 && p.rowg.tiles(shape->max_new) >= 1 << 28) p.rowg.max_units = 9;
     p.cuts = reinterpret_cast<CutRecord*>(ws + w.cut_off);
     p.part = reinterpret_cast<float*>(ws + w.mass_part_off);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -82,11 +82,12 @@ static inline PagedLayout paged_layout(const seka_paged_shape* s) {
 #ifdef __CUDACC__
 
 // Records an argument that only the device could see to be wrong.
-__device__ __forceinline__ void report_invalid(int* status, int where) {
-    if (atomicCAS(status, (int)SEKA_OK, (int)SEKA_ERR_INVALID_ARG) == (int)SEKA_OK) status[1] = where;
+__device__ __forceinline__ void report(int* status, seka_status what, int where) {
+    if (atomicCAS(status, (int)SEKA_OK, (int)what) == (int)SEKA_OK) status[1] = where;
 }
+__device__ __forceinline__ void report_invalid(int* status, int where) { report(status, SEKA_ERR_INVALID_ARG, where); }
 // codes of status[1]
-constexpr int kWhereSeq = 200, kWherePage = 201;
+constexpr int kWhereSeq = 200, kWherePage = 201, kWhereSteps = 202;
 
 __device__ __forceinline__ PagedSeq load_seq(const PagedView& v, int b) {
     const PagedSeq s = paged_seq(v, b);

@@ -7,7 +7,7 @@
 // itself and finds where its share begins.  What a unit and a step are is the geometry's to say:
 //   units(L, n)      units of a sequence with L cached tokens, the last n of them new, per KV head
 //   steps(L, n, u)   steps of its unit u (at least 1)
-//   max_units        no sequence has more units (from what the host knows)
+//   max_units        no sequence has more units (from what the host knows); more than 8 where the steps of so many could pass 31 bits
 #pragma once
 
 #include "seka_paged.cuh"
@@ -19,7 +19,7 @@ namespace seka {
 struct StepGeo {
     int tp, shift;
     int min_share;      // steps that a share has at least
-    int max_units;
+    int max_units;      // (2^24 steps of 128 tokens each at most: eight fit 31 bits)
     SEKA_HD int steps_to(int L, int n, int last) const {
         const int x = L - n + last;
         return x <= (1 << shift) ? 1 : (int)(((long long)x + (1 << shift) - 1) >> shift);
@@ -51,6 +51,21 @@ struct RowGeo {
     SEKA_HD int steps(int L, int n, int u) const { return tiles(n) - first(L, n, u); }
 };
 
+// Steps of the units first, first + stride, .. of a sequence, per KV head.  A unit's steps fit 31 bits, their sum need not: a prompt of a million
+// tokens with 128 query heads on a KV head has more than 2^31.
+template <typename Sum = long long, typename Geo> SEKA_HD Sum steps_of_units(const Geo& g, int L, int n, int first, int stride) {
+    Sum t = 0;
+    for (int u = first, U = g.units(L, n); u < U; u += stride) t += g.steps(L, n, u);
+    return t;
+}
+// Steps of a full share of a line of `all` among n_cta.
+SEKA_HD long long share_of(long long all, int n_cta, int min_share) {
+    const long long share = (all + n_cta - 1) / n_cta;
+    return share < min_share ? min_share : share;
+}
+// Steps of a CTA, its segments' and the merge's sums are counted in 31 bits.  2^30 steps would take more than twenty minutes.
+constexpr long long kMaxShare = 1LL << 30;
+
 // A place on the line: step `j` of unit p of KV head h of sequence b.
 struct LinePos { int b, h, p, j; };
 
@@ -70,7 +85,8 @@ template <int NT> struct ShareScratch {
     long long warp_sum[NT / 32];
     long long rest;                     // steps into the KV head that the share begins in
     int b, L, n, h, p, j;
-    int len[NT], new_tokens[NT], steps[NT];
+    int len[NT], new_tokens[NT];
+    long long steps[NT];
 };
 
 // exclusive scan over the block; `all` receives the sum
@@ -107,36 +123,37 @@ __device__ inline Share find_share(const PagedView& v, const Geo& g, int n_cta, 
         const int b = b0 + tid;
         L = 0; n = 0;
         if (b < v.B) { const PagedSeq s = load_seq(v, b); L = s.L; n = s.n; }
-        int per = 0;
+        long long per = 0;
         if (g.max_units <= 8) {
-            const int U = b < v.B ? g.units(L, n) : 0;
-            for (int u = 0; u < U; ++u) per += g.steps(L, n, u);
+            if (b < v.B) per = steps_of_units<int>(g, L, n, 0, 1);
         } else {
             sc.len[tid] = L; sc.new_tokens[tid] = n;
             __syncthreads();
             for (int k = warp; k < NT && b0 + k < v.B; k += NT / 32) {
-                const int Lk = sc.len[k], nk = sc.new_tokens[k], U = g.units(Lk, nk);
-                int t = 0;
-                for (int u = lane; u < U; u += 32) t += g.steps(Lk, nk, u);
-                t = __reduce_add_sync(0xffffffffu, t);
+                long long t = steps_of_units(g, sc.len[k], sc.new_tokens[k], lane, 32);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
                 if (lane == 0) sc.steps[k] = t;
             }
             __syncthreads();
             if (b < v.B) per = sc.steps[tid];
         }
-        mine = (long long)per * v.Hkv;
+        mine = per * v.Hkv;
     };
     long long total = 0, all;
     for (int b0 = 0; b0 < v.B; b0 += NT) { count(b0); total += mine; }
     block_scan<NT>(total, sc.warp_sum, all);
-    long long share = (all + n_cta - 1) / n_cta;
-    if (share < g.min_share) share = g.min_share;
+    const long long share = share_of(all, n_cta, g.min_share);
     Share r;
     r.share = (int)share;
     const long long x = share * cta;
     r.len = all - x < share ? all - x : share;
     r.at = LinePos{0, 0, 0, 0};
-    if (r.len <= 0) { r.len = 0; return r; }            // (the same for the whole block)
+    if (r.len <= 0 || share > kMaxShare) {              // (the same for the whole block; too long: for all blocks)
+        if (share > kMaxShare) report(v.status, SEKA_ERR_UNSUPPORTED, kWhereSteps);
+        r.len = 0;
+        return r;
+    }
     long long before = 0;
     for (int b0 = 0; b0 < v.B; b0 += NT) {
         if (v.B > NT) count(b0);
@@ -187,7 +204,7 @@ struct Segment {
 };
 struct Walk {
     LinePos at;
-    int left, first;        // (a share is below 2^31 steps: a line of 2^31 steps of 128 keys would take hours)
+    int left, first;        // (a share is at most kMaxShare)
     int q0, L, n;
 };
 __device__ __forceinline__ void walk_load(const PagedView& v, Walk& w) {

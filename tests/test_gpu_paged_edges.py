@@ -81,3 +81,82 @@ def test_the_exponential_of_every_column():
     out.fill_(float("nan"))
     binding.seka_attention_mass(c.shape, c.Q, c.K, lse, None, out, c.ws)
     assert c.status() == binding.SEKA_OK and (out[:, 0, :old + n] == 0).all()
+
+
+def test_more_than_2_31_steps_of_a_sequence():
+    # 128 query heads on one KV head: 270336 new tokens over a cache of 2.3 million rows are 2.4e9 steps of attention (units of two tokens) and as
+    # many of the weights.  The cache repeats eight pages, so that the sums over a token's keys are sums over 2048 rows and how often
+    # it sees each.
+    G, d, page, period = 128, 64, 256, 2048
+    L, n = 9000 * page - 3, 270336
+    cap, old = 9000 * page, L - n
+    attn_steps = sum((old + 2 * u + 2 + 127) // 128 for u in range(n // 2))
+    mass_steps = sum(n - max(0, 256 * u - old) for u in range(cap // 256))
+    assert attn_steps > 1 << 31 and mass_steps > 1 << 31
+    g = torch.Generator(device="cuda").manual_seed(42)
+    K, V = (torch.randn((8, page, 1, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    V += 1
+    Q = torch.randn((n, G, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    table = (torch.arange(9000, dtype=torch.int32, device="cuda") % 8).view(1, -1).contiguous()
+    lens = torch.tensor([L], dtype=torch.int32, device="cuda")
+    shape = binding.make_paged_shape(batch=1, max_new=n, total_new=n, n_q_heads=G, n_kv_heads=1, head_dim=d, page_size=page, n_pages=8,
+                                     block_table=table, cache_lens=lens)
+    ws = binding.new_paged_workspace(shape)
+    O, lse = torch.full_like(Q, float("nan")), torch.full((n, G), float("nan"), device="cuda")
+    binding.seka_paged_attention(shape, Q, K, V, O, lse, ws)
+    assert binding.seka_poll_status(ws) == binding.SEKA_OK
+    assert bool(torch.isfinite(lse).all()) and bool(torch.isfinite(O).all())
+    k, v, at = K.view(period, d).double(), V.view(period, d).double(), torch.arange(period, device="cuda")
+    t = torch.cat([torch.tensor([0, 1, 2, n - 2, n - 1]), torch.randint(0, n, (60,), generator=torch.Generator().manual_seed(1))]).cuda()
+    often = ((old + t)[:, None] - at[None, :]).div(period, rounding_mode="floor").double() + 1            # rows j = at (mod 2048) up to old + t
+    s = Q[t].double() @ k.T / math.sqrt(d)                                                               # [tokens, heads, 2048]
+    ref_lse = torch.logsumexp(s + often.log()[:, None], 2)
+    p = torch.exp(s - ref_lse[..., None]) * often[:, None]
+    ref, A = p @ v, p @ v.abs()
+    dq = (Q[t].double().abs() @ k.abs().T / math.sqrt(d)).amax(2)
+    delta = d * 2.0 ** -23 * dq
+    # Beside the bounds of the other sizes: a row's sum takes 18000 steps, off by at most 2^-24 of it each; its output 16 keys
+    # at a time, 144000 additions inside the tensor core of at most 2^-23 of the sum of magnitudes each.
+    steps = cap // 128
+    assert ((lse[t].double() - ref_lse).abs() <= delta + 2.0 ** -17 + 2.0 ** -21 * ref_lse.abs() + steps * 2.0 ** -24).all()
+    err = (O[t].double() - ref).abs()
+    tol = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * delta[..., None] + 2.0 ** -16 + steps * 2.0 ** -24 + 8 * steps * 2.0 ** -23) * A
+    assert (err <= tol).all(), float((err / tol).max())
+    del O
+    out = torch.full((1, 1, cap), float("nan"), device="cuda")
+    binding.seka_attention_mass(shape, Q, K, lse, None, out, ws)
+    assert binding.seka_poll_status(ws) == binding.SEKA_OK
+    assert bool(torch.isfinite(out[0, 0, :L]).all())
+    keys = torch.tensor([0, 1, 255, 256, 70000, old - 1, old, old + 1, old + 1000, old + n // 2, L - 5000, L - 2], device="cuda")
+    ref = torch.zeros(len(keys), dtype=torch.float64, device="cuda")
+    for t0 in range(0, n, 8192):
+        w = torch.exp(Q[t0:t0 + 8192].double() @ k[keys % period].T / math.sqrt(d) - lse[t0:t0 + 8192].double()[..., None]).sum(1)
+        ref += w.masked_fill(keys[None, :] > (old + torch.arange(t0, min(t0 + 8192, n), device="cuda"))[:, None], 0.0).sum(0)
+    # eight sums side by side of up to 270336 x 128 / 8 terms of about the same size: off by 2^-24 of the sum each at the very most, which
+    # would be a quarter; roundings of both signs leave the square root of that many, 2^-24 sqrt(4.3e6) = 1.2e-4, here with a factor of 32
+    err = (out[0, 0, keys].double() - ref).abs()
+    assert (err <= (delta.max() * 2 + 2.0 ** -16 + 32 * 1.3e-4) * ref).all(), float((err / ref).max())
+
+
+def test_work_beyond_what_a_cta_counts_is_refused():
+    # 20000 new tokens with 128 query heads over the longest cache: more than 2^30 steps a CTA; nothing is computed
+    G, d, page, n = 128, 64, 256, 20000
+    pages = 0x7fff0000 // page
+    assert sum((0x7fff0000 - n + 2 * u + 2 + 127) // 128 for u in range(n // 2)) > 148 << 30
+    K = torch.zeros((1, page, 1, d), dtype=torch.bfloat16, device="cuda")
+    Q = torch.zeros((n, G, d), dtype=torch.bfloat16, device="cuda")
+    table, lens = torch.zeros((1, pages), dtype=torch.int32, device="cuda"), torch.tensor([0x7fff0000], dtype=torch.int32, device="cuda")
+    shape = binding.make_paged_shape(batch=1, max_new=n, total_new=n, n_q_heads=G, n_kv_heads=1, head_dim=d, page_size=page, n_pages=1,
+                                     block_table=table, cache_lens=lens)
+    ws = binding.new_paged_workspace(shape)
+    O, lse = torch.full_like(Q, 3.0), torch.full((n, G), 3.0, device="cuda")
+    binding.seka_paged_attention(shape, Q, K, K, O, lse, ws)
+    assert binding.seka_poll_status(ws) == binding.SEKA_ERR_UNSUPPORTED
+    assert bool((O == 3.0).all()) and bool((lse == 3.0).all())
+    # the same launch on a shorter cache
+    binding.seka_reset_status(ws)
+    lens.fill_(n)
+    binding.seka_paged_attention(shape, Q, K, K, O, lse, ws)
+    assert binding.seka_poll_status(ws) == binding.SEKA_OK
+    want = torch.arange(1, n + 1, device="cuda").double().log()[:, None]
+    assert bool((O == 0).all()) and bool(((lse.double() - want).abs() <= 2.0 ** -17 + 2.0 ** -21 * want).all())

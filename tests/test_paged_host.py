@@ -242,3 +242,66 @@ def test_counts_beyond_their_bits_are_refused(lib):
         assert lib.seka_paged_workspace_bytes(ctypes.byref(s)) == 0
         for call in (append, attend, mass, evict):
             assert call(lib, s) == binding.SEKA_ERR_UNSUPPORTED, (bad, call)
+
+
+SUMS = r'''
+#include <stdio.h>
+#include "seka_paged_sched.cuh"
+using namespace seka;
+int main() {
+    int bad = 0;
+    auto expect = [&](bool ok, int line) { if (!ok && bad++ < 5) printf("line %d\n", line); };
+    // the steps of a sequence against sums in 128 bits in closed form: a unit's last token sees L - n + last keys, every 2^shift are a step
+    auto floors = [](__int128 count, __int128 a, __int128 b, __int128 m) {          // sum of (a i + b) / m over i < count
+        __int128 t = 0;
+        while (true) {
+            t += (a / m) * count * (count - 1) / 2 + (b / m) * count;
+            a %= m; b %= m;
+            const __int128 top = a * count + b;
+            if (top < m) return t;
+            count = top / m; b = top % m;
+            const __int128 x = m; m = a; a = x;
+        }
+    };
+    const int cases[][3] = {{1100000, 1100000, 2}, {2304000, 270336, 2}, {4300000, 4300000, 32}, {6000000, 6000000, 64}, {2000000, 1900001, 4}, {300000, 299999, 2},
+                            {40000000, 3000000, 2}, {1000, 1000, 16}};
+    for (const auto& c : cases) {
+        const int L = c[0], n = c[1], tp = c[2];
+        const StepGeo g = {tp, 7, 4, 0};
+        const int U = g.units(L, n);
+        expect(U == (n + tp - 1) / tp, __LINE__);
+        __int128 want = floors(U - 1, tp, (__int128)L - n + tp + 127, 128) + (L + 127) / 128;
+        long long got = 0;
+        for (int lane = 0; lane < 32; ++lane) got += steps_of_units(g, L, n, lane, 32);
+        expect((__int128)got == want && got == steps_of_units(g, L, n, 0, 1), __LINE__);
+        const RowGeo r = {tp / 2, 8, 2, 0};
+        const int V = r.units(L, n), T = r.tiles(n);
+        __int128 rows = 0;
+        for (int u = 0; u < V; ++u) { const long long x = 256LL * u - (L - n); rows += T - (x > 0 ? x / r.tp : 0); }
+        got = 0;
+        for (int lane = 0; lane < 32; ++lane) got += steps_of_units(r, L, n, lane, 32);
+        expect((__int128)got == rows, __LINE__);
+    }
+    expect(steps_of_units(StepGeo{2, 7, 4, 0}, 1100000, 1100000, 0, 1) > 0x7fffffffLL, __LINE__);
+    // shares cover the line, and what a CTA cannot count is above the limit
+    for (long long all : {1LL, 3LL, 4LL, 147LL * 4, 1LL << 31, (1LL << 32) + 5, 148LL << 30, (148LL << 30) + 1, 1LL << 44})
+        for (int ctas : {1, 7, 148, 444}) {
+            const long long s = share_of(all, ctas, 4);
+            expect(s >= 4 && s * ctas >= all && (s == 4 || (s - 1) * ctas < all), __LINE__);
+        }
+    expect(share_of(148LL << 30, 148, 4) == kMaxShare && share_of((148LL << 30) + 1, 148, 4) > kMaxShare, __LINE__);
+    // the merge: parts of the longest unit in shares at the limit
+    const int n = 0x7fff0000 / 64, j = 1;
+    expect((long long)n - j + kMaxShare - 1 <= 0x7fffffffLL, __LINE__);
+    return bad ? 1 : 0;
+}
+'''
+
+
+def test_sums_of_steps_on_the_host(tmp_path):
+    src, exe = tmp_path / "sums.cpp", tmp_path / "sums"
+    src.write_text(SUMS)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(build.NVCC)), "include")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", build.CSRC, "-I", cuda, str(src), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
