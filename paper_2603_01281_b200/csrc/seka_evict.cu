@@ -67,6 +67,8 @@ struct EvSmem {
     uint32_t warp_min[EV_WARPS], warp_max[EV_WARPS];
     int found[4];
 };
+constexpr size_t EV_MAX_BYTES = sizeof(EvSmem) + (size_t)EV_MAX_CACHED * 5;
+static_assert(EV_MAX_BYTES <= 227 * 1024, "shared memory");
 
 __device__ __forceinline__ int ld_cluster(const int* local, int rank) {
     uint32_t a;
@@ -503,7 +505,9 @@ extern "C" seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_p
     // longer: ranks are formed again in every pass (one context of 65536 that way: 78 us, 56 cached; 64 of 1024 to 4096: 92 and 80)
     p.cached = rows <= EV_MAX_CACHED ? (int)rows : 0;
     const size_t bytes = sizeof(EvSmem) + (size_t)p.cached * 5;
-    if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return SEKA_ERR_CUDA;
+    // the limit belongs to the function, not to the launch: always the most that any call asks for, so that a call of another host thread
+    // between this line and the launch does not lower it
+    if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)EV_MAX_BYTES) != cudaSuccess) return SEKA_ERR_CUDA;
     stc = launch_cluster(true, (unsigned)p.cluster, evict_select_kernel, dim3(pairs * (unsigned)p.cluster), EV_THREADS, bytes, st, p);
     if (stc != SEKA_OK) return stc;
     const int D = shape->head_dim;

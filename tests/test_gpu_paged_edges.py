@@ -1,5 +1,8 @@
 """Edges of the paged calls: NaN among the queries of the accumulated weights and the exponential of every column."""
+import ctypes
 import math
+import sys
+import threading
 
 import pytest
 import torch
@@ -160,3 +163,45 @@ def test_work_beyond_what_a_cta_counts_is_refused():
     assert binding.seka_poll_status(ws) == binding.SEKA_OK
     want = torch.arange(1, n + 1, device="cuda").double().log()[:, None]
     assert bool((O == 0).all()) and bool(((lse.double() - want).abs() <= 2.0 ** -17 + 2.0 ** -21 * want).all())
+
+
+def test_evictions_of_several_host_threads():
+    # caches of very different lengths side by side: the selections ask for 200 KB of shared memory and for 34 KB
+    def cache(lens, seed):
+        c = R.Cache(lens, [0] * len(lens), 1, 1, 64, 256, seed=seed)
+        c.m = torch.rand((c.B, 1, c.cap), generator=c.g).cuda()
+        c.p = torch.arange(c.cap, dtype=torch.int32).expand(c.B, 1, -1).contiguous().cuda()
+        c.mo, c.po, c.lo = torch.empty_like(c.m), torch.empty_like(c.p), torch.empty_like(c.lens_d)
+        return c
+
+    caches = [cache([290000], 43), cache([300, 20], 44), cache([280000], 45), cache([400], 46)]
+    streams = [torch.cuda.Stream() for _ in caches]
+    call, begin, seen = binding.load().seka_evict_cache, threading.Barrier(len(caches)), [set() for _ in caches]
+
+    def cut(c, stream, statuses):
+        torch.cuda.set_device(0)
+        args = (ctypes.byref(c.shape), *(x.data_ptr() for x in (c.K, c.V, c.m, c.mo, c.p, c.po)), None, 0, c.lens_d.data_ptr(), 200, 10,
+                c.lo.data_ptr(), c.ws.data_ptr(), c.ws.numel(), stream.cuda_stream)
+        begin.wait(timeout=60)
+        for _ in range(4000):
+            statuses.add(call(*args))
+
+    torch.cuda.synchronize()
+    every = sys.getswitchinterval()
+    sys.setswitchinterval(1e-5)
+    try:
+        threads = [threading.Thread(target=cut, args=a) for a in zip(caches, streams, seen)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        sys.setswitchinterval(every)
+    torch.cuda.synchronize()
+    assert seen == [{binding.SEKA_OK}] * len(caches), seen
+    for c in caches:
+        assert c.status() == binding.SEKA_OK and c.lo.tolist() == [min(l, 200) for l in c.lens]
+    for c in caches[1::2]:                      # (the long ones are compared elsewhere)
+        kept = R.evict(c, c.m, c.p, None, c.lens_d, 200, 10)
+        for b in range(c.B):
+            assert c.po[b, 0, :min(c.lens[b], 200)].tolist() == kept[b][0]
