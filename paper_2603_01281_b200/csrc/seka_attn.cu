@@ -1034,9 +1034,10 @@ static seka_status launch_attn_t(const TileMaps& tm, const AttnParams& p, cudaSt
         if (p.sched.pair_heads && p.sched.n_items_max <= (long long)n_sm && p.sched.n_qt > 1 && p.sched.n_qt <= most)
             kern = seka_attn_fwd_kernel<D, OutT, TABLE, true>;
     }
-    // the attribute belongs to the function on the current device: set on every call (a cheap driver call), so that a
-    // process that drives several devices, or calls from several threads, needs no bookkeeping here
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != cudaSuccess) return SEKA_ERR_CUDA;
+    // the attribute belongs to the function on the current device: set on every call (a cheap driver call), so that a process that
+    // drives several devices needs no bookkeeping here; always to the same value, so that a call of another host thread with a smaller
+    // `dyn`, between this line and the launch, does not lower it
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_LIMIT) != cudaSuccess) return SEKA_ERR_CUDA;
     // persistent CTAs, one per SM (the kernel needs the whole SM: all of tensor memory and most of shared memory)
     const unsigned grid = (unsigned)(p.sched.n_items_max < (long long)n_sm ? p.sched.n_items_max : (long long)n_sm);
     if (grid == 0) return SEKA_OK;

@@ -1307,8 +1307,11 @@ static seka_status launch_tiles_t(TileArgs& a, long long n_units, size_t smem, i
     if (!device_info(&n_sm)) return SEKA_ERR_CUDA;
     auto kern = edit_tiles_kernel<D, SIDE, KT, PACK, NTH>;
     constexpr int CTAS = EtSmem<D, SIDE, PACK>::CTAS;
-    if (smem > 220 * 1024) return SEKA_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SEKA_ERR_CUDA;
+    // the same limit for every call: it belongs to the function, and another host thread may call between it and the launch (the
+    // stand-alone form has 8 KB of its own)
+    constexpr int most = (SIDE ? 220 : 218) * 1024;
+    if (smem > most) return SEKA_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return SEKA_ERR_CUDA;
     long long per_sm = (227 * 1024) / (smem + (SIDE ? 4 : 9) * 1024);
     per_sm = per_sm > CTAS ? CTAS : (per_sm < 1 ? 1 : per_sm);
     // one wave; a multiple of the KV heads or (routed) of the (sequence, KV head) pairs
@@ -1772,8 +1775,8 @@ static seka_status launch_stage_pipe(const seka_shape* s, const WorkspaceLayout&
         alpha = route.alpha_out;
     }
     const size_t route_smem = n_route > 0 ? route_smem_bytes(D, s->n_experts, route.k_route) : 0;       // (at most 34 KB, on top of 19 of its own)
-    if (route_smem > 24 * 1024 &&
-        cudaFuncSetAttribute(prep_projector_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)route_smem) != cudaSuccess) return SEKA_ERR_CUDA;
+    if (route_smem > 24 * 1024 &&       // always the same limit: see launch_tiles_t
+        cudaFuncSetAttribute(prep_projector_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxRouteSmem) != cudaSuccess) return SEKA_ERR_CUDA;
     seka_status stc = launch_kernel(true, prep_projector_kernel, (unsigned)(n_p + n_flag + n_route + jobs.n_items_blocks + jobs.n_conv_blocks), PREP_THREADS,
                                     route_smem, st, U, mask,
                                     static_cast<__nv_bfloat16*>(P), tile_hot, reinterpret_cast<uint8_t*>(ws + w.info_off), s->batch,

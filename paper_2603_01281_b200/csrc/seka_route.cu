@@ -17,7 +17,7 @@ seka_status launch_route(const seka_shape* shape, const void* Q, const float* U,
                          float* alpha_out, cudaStream_t stream) {
     const size_t smem = route_smem_bytes(shape->head_dim, shape->n_experts, k_route);
     if (smem > 48 * 1024 &&      // very wide banks of rank-1 experts: up to 66 KB
-        cudaFuncSetAttribute(route_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        cudaFuncSetAttribute(route_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxRouteSmem) != cudaSuccess)
         return SEKA_ERR_CUDA;
     // one pair's latency where every pair has an SM to itself, throughput otherwise (408 pairs of four experts
     // of rank 64 at head_dim 128 in 13.7 us, at 64 in 8.4)

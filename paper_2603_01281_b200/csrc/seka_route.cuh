@@ -22,6 +22,9 @@ __host__ __device__
 static inline size_t route_smem_bytes(int D, int M, int k_route) {
     return sizeof(double) * ((size_t)D + (size_t)M * k_route * route_chunks(M, k_route) + M);
 }
+// ... at most (rank x experts is at most 4096, and so is their product with the pieces): the limit that launches set, the same for every
+// call, because it belongs to the function and other host threads may call meanwhile
+constexpr size_t kMaxRouteSmem = sizeof(double) * (128 + 4096 + 4096);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float route_load_q(const void* Q, int q_is_f32, size_t idx) {
