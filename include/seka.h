@@ -320,6 +320,7 @@ seka_status seka_rope_append(const seka_paged_shape* shape, const seka_rope* rop
  * Attention of the new tokens over the paged cache: new token i of sequence b sees the rows j <= cache_lens[b] - n_b + i,
  *     O[t, hq, :] = sum_j softmax_j(Q[t, hq, :] . K[j, hq / (Hq/Hkv), :] * scale) V[j, hq / (Hq/Hkv), :]
  * Q and O are bf16 [T, Hq, d] (O may be Q), lse, if not NULL, fp32 [T, Hq] (natural log).  A token that sees no key gets O = 0, lse = -inf.
+ * Weights are rounded to bf16 for the product with V, as in seka_attention_fwd; scores, sums and outputs are fp32 until the store.
  * What pages hold behind the last cached token does not matter.  An infinity or NaN in a value row of the cache reaches the tokens
  * that see it and may reach earlier tokens of the same chunk too.
  */
@@ -330,7 +331,8 @@ seka_status seka_paged_attention(const seka_paged_shape* shape, const void* Q, c
  * Accumulated attention weight of the cached rows: with lse as seka_paged_attention gave it for the same queries and cache,
  *     mass_out[b, h, j] = (j < cache_lens[b] - n_b ? mass_in[b, h, j] : 0) + sum over the new tokens i that see j and the query
  *                         heads hq of KV head h of exp(Q[t, hq, :] . K[j, h, :] * scale - lse[t, hq])
- * for j < cache_lens[b] (new rows begin at zero).  fp32, summed in a fixed order.  mass_in == NULL: zeros; mass_out may be mass_in.
+ * for j < cache_lens[b] (new rows begin at zero).  fp32, summed in a fixed order.  A NaN in a query or its lse reaches the rows that its
+ * token sees, and no others.  mass_in == NULL: zeros; mass_out may be mass_in.
  */
 seka_status seka_attention_mass(const seka_paged_shape* shape, const void* Q, const void* K_pages, const float* lse,
                                 const float* mass_in, float* mass_out, void* workspace, size_t workspace_bytes, void* cuda_stream);

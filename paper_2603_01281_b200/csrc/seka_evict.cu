@@ -12,8 +12,9 @@
 //                         kept ones behind, every warp on consecutive rows so that ranks come from ballots.  Four rows a lane
 //                         at a time: with many pairs the passes are bound by instructions, not by memory.
 //   evict_move_kernel     copies K, V, weight and position of the kept rows behind into the freed rows.
-// 64 contexts of 1024 to 4096 rows, 8 KV heads of 128, cut to 2048: 80 us = 30 (selection) + 50 (233 MB in pieces of 256 bytes, 4.1 TB/s);
-// one of 65536 cut to 16384: 56 us = 27 (a chain of passes and cluster barriers) + 24.
+// 64 contexts of 1024 to 4096 rows, 8 KV heads of 128, cut to 2048: 80 us = 30 (selection) + 50 (233 MB, 4.1 TB/s: a chain of list, table and
+// row, four rows of a warp in flight); one of 65536 cut to 16384: 60 us, of which 27 are the selection (a chain of passes and cluster
+// barriers on 64 SMs) and 24 the moves.
 // What is kept below `keep` does not move: a cache that is cut often, by a little each time, moves only that little.  Sources lie at or
 // behind `keep`, destinations below it, so the copies need no order.
 #include <math.h>
@@ -497,12 +498,12 @@ extern "C" seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_p
     int n_sm = 0;
     if (!device_info(&n_sm)) return SEKA_ERR_CUDA;
     // CTAs of a pair: more while they still find SMs and have 2048 rows each (a cache may be filled to its last page).  One context of 65536
-    // rows: 56 us, 235 with one CTA a pair; 8 of 8192: 51 and 56.
+    // rows: 60 us, 239 with one CTA a pair; 8 of 8192: 51 and 55.
     p.cluster = 1;
     while (p.cluster < EV_MAX_CLUSTER && 2LL * p.cluster * pairs <= 2LL * n_sm && p.v.cap > 4 * 1024 * p.cluster) p.cluster *= 2;
     const int lanes = p.cluster * EV_WARPS * 128;
     const long long rows = ((long long)p.v.cap + lanes - 1) / lanes * (EV_WARPS * 128);     // most rows of a CTA
-    // longer: ranks are formed again in every pass (one context of 65536 that way: 78 us, 56 cached; 64 of 1024 to 4096: 92 and 80)
+    // longer: ranks are formed again in every pass (one context of 65536 that way: 82 us, 60 cached; 64 of 1024 to 4096: 92 and 80)
     p.cached = rows <= EV_MAX_CACHED ? (int)rows : 0;
     const size_t bytes = sizeof(EvSmem) + (size_t)p.cached * 5;
     // the limit belongs to the function, not to the launch: always the most that any call asks for, so that a call of another host thread
@@ -514,7 +515,7 @@ extern "C" seka_status seka_evict_cache(const seka_paged_shape* shape, void* K_p
     const long long most = p.v.cap - keep < keep ? p.v.cap - keep : keep;          // rows of a pair that can move
     const long long fill = (16LL * n_sm + pairs - 1) / pairs;
     // rows of a warp: eight while that leaves fewer than eight warps per SM, up to 32 (64 contexts 80 us, 86 with eight always; one of
-    // 1500 15.6, 17.6 with 32 always)
+    // 1500 14.2, 16.4 with 32 always; one of 65536 60, 58 with eight)
     p.move_rows = 32;
     while (p.move_rows > 8 && (long long)pairs * most < 8LL * n_sm * p.move_rows) p.move_rows /= 2;
     long long blocks = most > 0 ? (most + MV_WARPS * p.move_rows - 1) / (MV_WARPS * p.move_rows) : 1;

@@ -8,8 +8,9 @@
 //                         1024 to 4096 tokens, 32/8 heads of 128 (343 MB): 64 us, 5.3 TB/s; the floor is 53.
 //   mass_tile_kernel      more rows, on tcgen05: 2 x 128 cached tokens stay in shared memory, tiles of 128 query rows (new token r / G,
 //                         head r % G) pass by.  Bound by the exponentials (one per score, against 2 d flops).
-//                         2 x 1024 tokens over 6000 to 8192, 32/8 heads of 128: 165 us, of which 105 are exponentials at the rate of the
-//                         special-function unit (57 % busy; a quarter of them run on the multiply-add pipe instead).
+//                         2 x 1024 tokens over 6000 to 8192, 32/8 heads of 128: 169 us; all exponentials at the rate of the special-function
+//                         unit would take 105 (a quarter of them run on the multiply-add pipe instead; the unit is 59 % busy).  Two summing
+//                         warps a scheduler, each a chain of multiply-add, exponential and sum, mostly wait for their own results.
 //   mass_merge_kernel     adds the parts of a unit that a share boundary cut.
 #include <math.h>
 
@@ -538,6 +539,10 @@ extern "C" seka_status seka_attention_mass(const seka_paged_shape* shape, const 
     p.Q = static_cast<const __nv_bfloat16*>(Q); p.lse = lse; p.mass_in = mass_in; p.mass_out = mass_out;
     const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / sqrtf((float)D);
     p.scale_log2 = scale * kLog2e;
+    // Steps that a share has at least.  Few rows, one sequence of 128 / 777 / 2048 / 4096 tokens on 8 KV heads, launched and waited for: from one
+    // on 19.0 / 19.0 / 19.6 / 20.2 us, from two 19.0 / 19.8 / 19.4 / 20.0, from four 19.8 / 20.6 / 20.3 / 20.6, from eight 23.0 / 22.2 / 21.6 /
+    // 21.7; one behind the other all 8.0, the call's work on the host.  Tiles, 32 new tokens over 1024: from one on 11.7 us, from two 13.4,
+    // from four 17.0; 128 over 4096 17.0 / 16.9 / 16.3; 512 over 2048 24.7 in each.
     p.key = KeyGeo{6, 4, 1};
     p.rowg = RowGeo{128 / G, 8, 2, (p.v.cap + 255) / 256};
     if (p.rowg.max_units <= 8 && p.rowg.tiles(shape->max_new) >= 1 << 28) p.rowg.max_units = 9;

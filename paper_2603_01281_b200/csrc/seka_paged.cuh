@@ -39,7 +39,7 @@ SEKA_HD int table_entry(const PagedView& v, int b, int j) { return v.table[(long
 
 // Attention and accumulated weights: up to this many rows (new tokens x query heads of a KV head) of a sequence the few-row kernel runs, else
 // the tile kernel.  It takes all that the few-row kernels hold: with 16 rows and 64 contexts of 1024 to 4096 tokens, 32/8 heads of 128,
-// attention takes 126 us (tiles 133), weights 66 (164); one context of 4096 22 (30) and 8 (16).
+// attention takes 127 us (tiles 150), weights 66 (163); one context of 4096 16.7 (19.9) and 7.8 (14.9).
 constexpr int kFewRows = 16;
 static inline bool few_rows(const seka_paged_shape* s) {
     return (long long)s->max_new * (s->n_q_heads / s->n_kv_heads) <= kFewRows;

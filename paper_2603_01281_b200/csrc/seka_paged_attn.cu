@@ -6,7 +6,8 @@
 //                         the scores of all rows with mma.sync m16n8k16 (16 rows are too few for a tcgen05 tile), keep
 //                         a private online softmax and P V in registers.  The CTA walks its equal share of all stages, unit after
 //                         unit, without the ring running dry between them.
-//                         64 contexts of 1024 to 4096 tokens, 32/8 heads of 128 (666 MB): 112 us, 5.9 TB/s; the floor is 103.
+//                         64 contexts of 1024 to 4096 tokens, 32/8 heads of 128 (666 MB): 112 to 116 us from device to device, 5.7 to 5.9
+//                         TB/s; the floor is 103.
 //   paged_merge_kernel    merges the parts of a unit that a share boundary cut: some 3 us of a single sequence's 11, four trips to memory.
 // Weights are rounded to bf16 for P V (half a step, 2^-8 of each); scores, sums and outputs stay in fp32 until the store.
 #include <math.h>
@@ -427,7 +428,8 @@ extern "C" seka_status seka_paged_attention(const seka_paged_shape* shape, const
     p.scale_log2 = scale * 1.4426950408889634f;
     p.tile_tokens = few ? shape->max_new : 128 / G;
     // one tile of rows at most per sequence and KV head: units of one tile (SHARED tile kernel), else of two.  64 contexts of 2048 on 16 heads
-    // of 64, 17 / 128 new tokens each: 184 / 186 us in units of two, 160 / 164 in units of one; 256 new tokens 228 / 249.
+    // of 64, 17 / 128 new tokens each: 178 / 184 us in units of two, 158 / 165 in units of one; 256 new tokens 253 / 297.  On 32/8 heads of
+    // 128, 32 new tokens 134 / 123.
     p.geo.tp = few ? shape->max_new : shape->max_new <= p.tile_tokens ? p.tile_tokens : 2 * p.tile_tokens;
     p.geo.shift = few ? 6 : 7;
     // A share is worth a CTA of its own from two stages of 64 tokens on (one sequence of 128 / 777 / 2048 / 4096 tokens, 8 KV heads, in a graph: 7.8 /

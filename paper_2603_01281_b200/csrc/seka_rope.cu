@@ -8,10 +8,10 @@
 // into shared memory.  A lane owns 16 elements of a head, as eight pairs where it can:
 //   NEIGHBOURS  interleaved pairs: 16 consecutive elements, any r (also what is not rotated at all);
 //   HALVES      pairs r/2 apart with r a multiple of 16: eight elements and their eight partners, both on 16-byte boundaries;
-//   STAGED      pairs r/2 apart at no alignment: the warp's rows go through shared memory, a lane per pair there (16384 tokens of
-//               32/8 heads of 128: 103 us where HALVES took 88).
+//   STAGED      pairs r/2 apart at no alignment: the warp's rows go through shared memory, a lane per pair there, three warp barriers a
+//               row (16384 tokens of 32/8 heads of 128, r = 126 / 22 / 2: 101 / 89 / 90 us, HALVES at r = 128 81).
 // The loads of the first rows are issued before the token's sequence, page and angles are known (100 -> 88 us); three groups of rows are in flight
-// as bf16, two as fp32.  16384 tokens of 32/8 heads of 128 in bf16 (403 MB): 82 us, 4.9 TB/s; some 16000 tokens of 16/16 heads of 64 in fp32
+// as bf16, two as fp32.  16384 tokens of 32/8 heads of 128 in bf16 (403 MB): 81 us, 5.0 TB/s; some 16000 tokens of 16/16 heads of 64 in fp32
 // (313 MB): 56 us, 5.6 TB/s; 64 tokens: 6.3 us on the device, less than the call's work on the host.
 #include "seka_kernels.h"
 #include "seka_paged.cuh"
