@@ -1,4 +1,5 @@
-"""Edges of the paged calls: NaN among the queries of the accumulated weights and the exponential of every column."""
+"""Edges of the paged calls: NaN among the queries of the accumulated weights and the exponential of every column, more than 2^31 steps, host
+threads side by side, more sequences than threads.  Tolerances are those of test_gpu_paged.py where nothing else is said."""
 import ctypes
 import math
 import sys
@@ -10,6 +11,7 @@ import torch
 from paper_2603_01281_b200 import binding
 
 import paged_ref as R
+from test_gpu_paged import attend, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -205,3 +207,24 @@ def test_evictions_of_several_host_threads():
         kept = R.evict(c, c.m, c.p, None, c.lens_d, 200, 10)
         for b in range(c.B):
             assert c.po[b, 0, :min(c.lens[b], 200)].tolist() == kept[b][0]
+
+
+@pytest.mark.parametrize("B,new,Hq,Hkv,d,page", [(330, (1, 1), 8, 2, 64, 16), (400, (1, 30), 8, 2, 64, 16), (790, (0, 150), 16, 1, 128, 32), (1200, (0, 3), 4, 1, 64, 16)])
+def test_more_sequences_than_threads(B, new, Hq, Hkv, d, page):
+    # the shares are found sequences by thread, a block's worth at a time: some batches that take several turns, up to eight units a sequence and
+    # more, sequences without new tokens and without any token among them
+    g = torch.Generator().manual_seed(47)
+    n = torch.randint(new[0], new[1] + 1, (B,), generator=g).tolist()
+    n[B // 2] = new[1]
+    old = torch.randint(0, 90, (B,), generator=g).tolist()
+    lens = [0 if i % 37 == 5 else a + b for i, (a, b) in enumerate(zip(n, old))]
+    c = R.Cache(lens, n, Hq, Hkv, d, page, seed=48)
+    O, lse = attend(c)
+    check_attention(c, O, lse)
+    ref, err = R.mass(c, lse)
+    out = torch.full((B, Hkv, c.cap), -7.0, device="cuda")
+    binding.seka_attention_mass(c.shape, c.Q, c.K, lse, None, out, c.ws)
+    assert c.status() == binding.SEKA_OK
+    inside = (torch.arange(c.cap, device="cuda")[None] < c.lens_d[:, None])[:, None].expand_as(out)
+    tol = d * 2.0 ** -23 * err + (2.0 ** -16 + (c.G * max(n) + 2) * 2.0 ** -24) * ref + 1e-30
+    assert (((out.double() - ref).abs() <= tol) | ~inside).all() and (out[~inside] == -7.0).all()
